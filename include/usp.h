@@ -326,6 +326,111 @@ int usp_attn_bwd(const usp_problem* p, const void* q, const void* k, const void*
                  const float* lse, const void* d_o, void* dq, void* dk, void* dv, int rank_begin,
                  int rank_end, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Rotary positions.  A head's elements are turned in pairs (x_a, x_b) by the angle position * freq[j]:
+ *   y_a = m (x_a cos - x_b sin),  y_b = m (x_a sin + x_b cos),   j = 0 .. rotary_dim/2 - 1,   m = magnitude;
+ * USP_ROPE_HALVES: a = j, b = j + rotary_dim/2;  USP_ROPE_PAIRS: a = 2j, b = 2j + 1.  Elements from rotary_dim on are
+ * copied.  The backward of it (backward != 0) is its transpose: the angle negated, the same m.  Angles are formed in 64
+ * bits (position * frequency in turns, of which the fraction counts), sines, cosines and products in 32. */
+typedef enum { USP_ROPE_HALVES = 0, USP_ROPE_PAIRS = 1 } usp_rope_layout;
+/* How the frequencies base^(-2j/rotary_dim) are changed for sequences longer than the model was trained on
+ * (arxiv 2309.00071, Sec. 3): LINEAR divides all by `factor`; BASE takes base * factor^(d/(d-2)), d = rotary_dim;
+ * BY_PARTS divides those that turn at most `alpha` times over original_len positions, keeps those that turn `beta`
+ * times or more, and blends in between, linearly in the number of turns. */
+typedef enum { USP_ROPE_UNSCALED = 0, USP_ROPE_LINEAR = 1, USP_ROPE_BASE = 2, USP_ROPE_BY_PARTS = 3 } usp_rope_scaling;
+typedef struct {
+  int32_t rotary_dim; /* multiple of 16, at most hs */
+  int32_t layout;     /* usp_rope_layout */
+  float magnitude;    /* m; the attention factor that goes with BY_PARTS is 0.1 ln(factor) + 1 */
+  int32_t reserved;
+  double freq[64];    /* radians per position; usp_rope_init fills it, a caller may have others (at most 1e6 each) */
+} usp_rope;
+
+/* Host only.  Fills *r.  factor > 0 is read with any scaling but UNSCALED; 0 <= alpha < beta and original_len >= 1 with
+ * BY_PARTS. */
+int usp_rope_init(usp_rope* r, int hs, int rotary_dim, int layout, double base, int scaling, double factor, double alpha,
+                  double beta, int64_t original_len, double magnitude);
+
+/* Rotary positions in the shards of virtual ranks [rank_begin, rank_end): q, q_out seq layout with hc heads, k, k_out seq
+ * layout with hk heads, whole-buffer base pointers; positions by Algorithm 2 (as usp_local_positions).  Before
+ * usp_attn_fwd; with backward != 0 on dq and dk after usp_attn_bwd.  Either pair may be NULL.  q_out may be q itself and
+ * k_out k; any other overlap of an output is rejected (USP_ERR_UNSUPPORTED).  Pointers on 16 bytes. */
+int usp_rope_shards(const usp_problem* p, const usp_rope* r, const void* q, const void* k, void* q_out, void* k_out,
+                    int backward, int rank_begin, int rank_end, void* stream);
+
+/* Rotary positions of `rows` tokens whose positions are given (DEVICE, int32, one per row; any value).  A row of q holds hq
+ * heads of hs elements side by side, rows are q_stride elements apart (so q may be columns of a QKV product's output);
+ * k, q_out and k_out likewise.  In place: same pointer and same stride; any other overlap of an output is rejected.  Either
+ * pair may be NULL, and rows = 0 does nothing.  Pointers and strides on 16 bytes, strides at least a row. */
+int usp_rope_rows(const usp_rope* r, const void* q, const void* k, void* q_out, void* k_out, const int32_t* positions,
+                  int64_t rows, int hq, int hk, int hs, int64_t q_stride, int64_t k_stride, int64_t q_out_stride,
+                  int64_t k_out_stride, int dtype, int backward, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * A cache of K and V in 8 bits, in pages of `page` tokens.  Codes are e4m3 (4 exponent bits, 3 of mantissa, no infinity);
+ * each page, KV head and tensor has one exponent byte x, and a code c stands for c * 2^(x - 127).
+ *   k_codes [pages][hk][page][hs];   v_codes [pages][hk][page/16][hs][16]: V in tiles of 16 tokens, transposed, so that the
+ *   second product of attention reads its operand as it lies;   k_scale, v_scale [pages][hk] exponent bytes.
+ * A request's tokens lie in the pages that its row of a block table names: token i in page table[i / page], place i % page. */
+typedef struct {
+  void* k_codes;
+  void* v_codes;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int64_t pages; /* pages * page < 2^31 */
+  int32_t page;  /* 16, 32, 64 or 128 */
+  int32_t hk, hs;
+  int32_t reserved;
+} usp_cache;
+#define USP_CACHE_MAX_REQUESTS 8192
+
+/* Block tables, slots and positions for the tokens that a step brings, on the device (so a captured step needs nothing of
+ * the host).  Request i of n has len_before[i] tokens in the first ceil(len_before[i] / page) pages of row i of block_table
+ * [n][max_pages], and gets rows cu_new[i] .. cu_new[i+1] of this step (cu_new [n+1] ascending from 0, at most total_new).
+ *   Pages that this takes more are the next ones of free_pages [n_free], in the order of the requests; their numbers are
+ *   written to the rows of the table.
+ *   len_after [n]; slots [total_new]: page number * page + place of each row; positions [total_new]: its position;
+ *   taken [2]: pages taken from the front of free_pages, and pages that were asked for.
+ * A request whose pages free_pages no longer holds, or whose row of the table is too short, gets none: its len_after is its
+ * len_before and its rows' slots are -1 (positions are given all the same).  Once pages have run out, every later request
+ * that needs one goes without.  Rows of no request (behind cu_new[n]) get slot -1 and position 0.  A row whose page number
+ * lies outside [0, pages) - as -1 for a page that another rank holds - gets slot -1 too.
+ * len_after must not be len_before, nor any output overlap an input (rejected where it is the same pointer).
+ * n_seqs at most USP_CACHE_MAX_REQUESTS; n_seqs = 0 or total_new = 0 are fine. */
+int usp_cache_extend(const int32_t* cu_new, const int32_t* len_before, int n_seqs, int64_t total_new, int32_t* block_table,
+                     int max_pages, int page, int64_t pages, const int32_t* free_pages, int64_t n_free, int32_t* len_after,
+                     int32_t* slots, int32_t* positions, int32_t* taken, void* stream);
+
+/* Writes K and V of `rows` tokens to their slots.  k, v: rows of hk heads of hs elements side by side, k_stride and v_stride
+ * elements apart (bf16 or fp32).  slots [rows]; a slot outside [0, pages * page) is skipped.
+ *   Per page, head and tensor, the exponent is the smallest with which every value lies within 448 * 2^e (within [-117, 96];
+ *   values beyond 448 * 2^96 are held at the largest code), at least what the page has already if tokens stand before the first
+ *   one written; where it grows, their codes are rounded again to the new exponent.  Writing place 0 starts a page anew.
+ *   Values are rounded to the nearest code, ties to even; NaN and infinities are held as NaN and do not count for e.
+ * Rows of one page have to stand together in `slots` (as usp_cache_extend gives them); stretches of ascending places are
+ * written one after the other.  Where they do not stand together the values of that page are undefined.  Places of a page
+ * behind those written are left as they were. */
+int usp_cache_append(const usp_cache* c, const void* k, const void* v, const int32_t* slots, int64_t rows, int64_t k_stride,
+                     int64_t v_stride, int dtype, void* stream);
+
+/* Attention of the rows of n_seqs requests over their cached tokens.  Request i has rows cu_q[i] .. cu_q[i+1] of q (cu_q [n+1]
+ * ascending, DEVICE), rows q_stride elements apart, hq heads of hs (bf16), head h reads KV head h / (hq/hk); kv_len[i] (DEVICE)
+ * tokens are in the cache, this step's among them, in the pages that row i of block_table [n_seqs][max_pages] names.
+ *   causal != 0: the request's rows are its last tokens, row j of m sees the first kv_len - m + j + 1; else all see all.
+ *   o [total_q][hq][hs] (o_dtype), lse [hq][total_q] float: normalised output and natural-log sum, as
+ *   usp_block_attn_fwd gives them for bs = 1 and Lq = total_q, so that usp_lse_merge joins results of ranks that hold
+ *   different pages: keys of a page whose number is outside [0, pages) are not seen.  A row that sees nothing gets o = 0 and
+ *   lse = -inf.  Rows of no request are left as they were.  What stands in the cache behind kv_len has no influence.
+ *   max_q: the most rows of any request, as far as the caller knows; only speed depends on it.  total_q = 0 or n_seqs = 0 does
+ *   nothing.  kv_len is taken as 0 .. max_pages * page.  scale = 0 means 1/sqrt(hs).
+ * The workspace (DEVICE, 16-byte aligned; its size depends on hq / hk, hs and max_q alone) holds partial results of the call;
+ * calls that overlap in time need one each.  Nothing in it has to be cleared or kept.  Results do not depend on the order in
+ * which workgroups finish. */
+size_t usp_cache_attn_workspace_bytes(const usp_cache* c, int hq, int max_q);
+int usp_cache_attn(const usp_cache* c, const void* q, int64_t q_stride, const int32_t* cu_q, const int32_t* kv_len,
+                   const int32_t* block_table, int max_pages, int n_seqs, int64_t total_q, int max_q, int hq, float scale,
+                   int causal, void* o, float* lse, int o_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 #if defined(USP_BUILDING)
 #pragma GCC visibility pop
 #endif

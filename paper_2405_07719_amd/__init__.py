@@ -20,6 +20,9 @@ USP_OK = 0
 USP_BF16, USP_FP32 = 0, 1
 USP_SPLIT_CONTIG, USP_SPLIT_ZIGZAG = 0, 1
 USP_SEQ_TO_HEAD, USP_HEAD_TO_SEQ, USP_SEQ_TO_HEAD_VT = 0, 1, 2
+USP_ROPE_HALVES, USP_ROPE_PAIRS = 0, 1
+USP_ROPE_UNSCALED, USP_ROPE_LINEAR, USP_ROPE_BASE, USP_ROPE_BY_PARTS = 0, 1, 2, 3
+USP_CACHE_MAX_REQUESTS = 8192
 USP_MAX_MERGE_PARTS = 64
 USP_MAX_RING_BLOCKS = 16
 
@@ -35,6 +38,16 @@ class usp_posdesc(C.Structure):
 
     def positions(self):
         return list(range(self.start0, self.start0 + self.len0)) + list(range(self.start1, self.start1 + self.len1))
+
+
+class usp_rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32),
+                ("freq", C.c_double * 64)]
+
+
+class usp_cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("pages", C.c_int64), ("page", C.c_int32), ("hk", C.c_int32), ("hs", C.c_int32), ("reserved", C.c_int32)]
 
 
 class UspError(RuntimeError):
@@ -104,6 +117,17 @@ def load():
     lib.usp_attn_bwd_workspace_bytes_with_ds.restype = C.c_size_t
     lib.usp_attn_bwd_workspace_bytes_with_ds.argtypes = [P(usp_problem), I]
     lib.usp_attn_bwd.argtypes = [P(usp_problem), V, V, V, V, V, V, V, V, V, I, I, V, C.c_size_t, V]
+    D = C.c_double
+    lib.usp_rope_init.argtypes = [P(usp_rope), I, I, I, D, I, D, D, D, L, D]
+    lib.usp_rope_shards.argtypes = [P(usp_problem), P(usp_rope), V, V, V, V, I, I, I, V]
+    lib.usp_rope_rows.argtypes = [P(usp_rope), V, V, V, V, V, L, I, I, I, L, L, L, L, I, I, V]
+    lib.usp_cache_extend.argtypes = [V, V, I, L, V, I, I, L, V, L, V, V, V, V, V]
+    lib.usp_cache_append.argtypes = [P(usp_cache), V, V, V, L, L, L, I, V]
+    lib.usp_cache_attn_workspace_bytes.restype = C.c_size_t
+    lib.usp_cache_attn_workspace_bytes.argtypes = [P(usp_cache), I, I]
+    lib.usp_cache_attn.argtypes = [P(usp_cache), V, L, V, V, V, I, I, L, I, I, F, I, V, V, I, V, C.c_size_t, V]
+    for name in ("usp_rope_init", "usp_rope_shards", "usp_rope_rows", "usp_cache_extend", "usp_cache_append", "usp_cache_attn"):
+        getattr(lib, name).restype = I
     for name in ("usp_ring_attn_bwd", "usp_ring_attn_fwd", "usp_validate", "usp_local_positions", "usp_layout_a2a", "usp_block_attn_fwd", "usp_lse_merge",
                  "usp_attn_fwd", "usp_attn_bwd", "usp_attn_delta", "usp_block_attn_bwd"):
         getattr(lib, name).restype = I
@@ -116,6 +140,17 @@ def _ptr(x):
         return None
     if isinstance(x, int):
         return x
+    return x.data_ptr()
+
+
+def _here(x):
+    """_ptr of a tensor that lies on the current device: the launch goes to that device's stream, and an address of another
+    one, or of the host, would be a fault there."""
+    if x is None or isinstance(x, int):
+        return x
+    device = x.get_device()
+    if device < 0 or device != (_raw_device() if _raw_device is not None else device):
+        raise ValueError(f"a tensor on {x.device} given to a launch on the current HIP device")
     return x.data_ptr()
 
 
@@ -311,3 +346,54 @@ def usp_attn_bwd(p, q, k, v, o, lse, d_o, dq, dk, dv, rank_begin, rank_end, work
     _check(load().usp_attn_bwd(C.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq),
                                _ptr(dk), _ptr(dv), rank_begin, rank_end, _ptr(workspace), workspace_bytes,
                                _stream(stream)), "usp_attn_bwd")
+
+
+def rope(hs, rotary_dim, layout, base, scaling=USP_ROPE_UNSCALED, factor=1.0, alpha=1.0, beta=32.0, original_len=0,
+         magnitude=1.0):
+    """A usp_rope for heads of hs elements, of which the first rotary_dim turn."""
+    r = usp_rope()
+    _check(load().usp_rope_init(C.byref(r), hs, rotary_dim, layout, base, scaling, factor, alpha, beta, original_len, magnitude),
+           "usp_rope_init")
+    return r
+
+
+def usp_rope_shards(p, r, q, k, q_out, k_out, backward, rank_begin, rank_end, stream=None):
+    _check(load().usp_rope_shards(C.byref(p), C.byref(r), _here(q), _here(k), _here(q_out), _here(k_out), int(bool(backward)),
+                                  rank_begin, rank_end, _stream(stream)), "usp_rope_shards")
+
+
+def usp_rope_rows(r, q, k, q_out, k_out, positions, rows, hq, hk, hs, q_stride, k_stride, q_out_stride, k_out_stride, dtype,
+                  backward, stream=None):
+    _check(load().usp_rope_rows(C.byref(r), _here(q), _here(k), _here(q_out), _here(k_out), _here(positions), rows, hq, hk, hs,
+                                q_stride, k_stride, q_out_stride, k_out_stride, dtype, int(bool(backward)), _stream(stream)),
+           "usp_rope_rows")
+
+
+def cache(k_codes, v_codes, k_scale, v_scale, pages, page, hk, hs):
+    """A usp_cache over the four tensors; it holds their addresses, not the tensors, which have to live as long as it is used."""
+    return usp_cache(_here(k_codes), _here(v_codes), _here(k_scale), _here(v_scale), pages, page, hk, hs, 0)
+
+
+def usp_cache_extend(cu_new, len_before, n_seqs, total_new, block_table, max_pages, page, pages, free_pages, n_free, len_after,
+                     slots, positions, taken, stream=None):
+    _check(load().usp_cache_extend(_here(cu_new), _here(len_before), n_seqs, total_new, _here(block_table), max_pages, page,
+                                   pages, _here(free_pages), n_free, _here(len_after), _here(slots), _here(positions),
+                                   _here(taken), _stream(stream)), "usp_cache_extend")
+
+
+def usp_cache_append(c, k, v, slots, rows, k_stride, v_stride, dtype, stream=None):
+    _check(load().usp_cache_append(C.byref(c), _here(k), _here(v), _here(slots), rows, k_stride, v_stride, dtype,
+                                   _stream(stream)), "usp_cache_append")
+
+
+def usp_cache_attn_workspace_bytes(c, hq, max_q):
+    return int(load().usp_cache_attn_workspace_bytes(C.byref(c), hq, max_q))
+
+
+def usp_cache_attn(c, q, q_stride, cu_q, kv_len, block_table, max_pages, n_seqs, total_q, max_q, hq, scale, causal, o, lse,
+                   o_dtype, workspace, workspace_bytes=None, stream=None):
+    if workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(load().usp_cache_attn(C.byref(c), _here(q), q_stride, _here(cu_q), _here(kv_len), _here(block_table), max_pages,
+                                 n_seqs, total_q, max_q, hq, scale, int(bool(causal)), _here(o), _here(lse), o_dtype,
+                                 _here(workspace), workspace_bytes, _stream(stream)), "usp_cache_attn")

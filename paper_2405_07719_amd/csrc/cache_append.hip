@@ -1,0 +1,268 @@
+// K and V rows into the pages of the 8-bit cache.
+//
+// HBM-bound: the values are read once, a third of their bytes or less are written.  A wave has one page, one KV head and one of
+// K and V: the rows of a page stand together in `slots`, so the wave that finds a row whose predecessor lies in another page
+// owns that page, its exponent byte and the tiles of V that the rows share with older tokens; nobody else writes there, and
+// no atomics or second pass over the cache are needed.  It walks the page in tiles of 16 tokens: the maximum over all of them,
+// then (again from the caches, or still in registers where there is one tile) the codes.
+//
+// A power of two as scale makes both steps exact but for the one rounding to e4m3: value * 2^-e is exact, and codes whose page
+// needs a larger exponent later are halved exactly, as long as they stay normal (2^-6 and more).
+#include <float.h>
+
+#include "serve_internal.h"
+
+namespace usp {
+namespace {
+
+constexpr int kThreads = 256;
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ inline f32x8 load8(const __bf16* p) { return __builtin_convertvector(*(const bf16x8*)p, f32x8); }
+__device__ inline f32x8 load8(const float* p) {
+  const f32x4 a = ((const f32x4*)p)[0], b = ((const f32x4*)p)[1];
+  return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+__device__ inline f32x2 load2(const __bf16* p) { return __builtin_convertvector(*(const bf16x2*)p, f32x2); }
+__device__ inline f32x2 load2(const float* p) { return *(const f32x2*)p; }
+
+__device__ inline float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
+
+// what a value counts towards the page's maximum: NaN and infinities nothing
+__device__ inline float magnitude_of(float x) {
+  const float y = fabsf(x);
+  return y <= FLT_MAX ? y : 0.0f;
+}
+
+// x / 2^e as the conversion takes it: NaN for NaN and infinities, at most the largest code
+__device__ inline float scaled(float x, float inv) {
+  const float y = x * inv, z = fabsf(y) > 448.0f ? copysignf(448.0f, y) : y;
+  return fabsf(x) <= FLT_MAX ? z : __int_as_float(0x7fc00000);
+}
+
+__device__ inline uint32_t codes4(float a, float b, float c, float d) {
+  int x = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, x, true);
+}
+
+// four codes at another exponent
+__device__ inline uint32_t recoded(uint32_t x, float by) {
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+  return codes4(lo[0] * by, lo[1] * by, hi[0] * by, hi[1] * by);
+}
+__device__ inline u32x4 recoded(u32x4 x, float by) {
+  return u32x4{recoded(x[0], by), recoded(x[1], by), recoded(x[2], by), recoded(x[3], by)};
+}
+
+// The smallest e with most <= 448 * 2^e = 1.75 * 2^(8 + e).
+__device__ inline int exponent_for(float most) {
+  const uint32_t bits = (uint32_t)__float_as_int(most);
+  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000);
+  return e < kCacheMinExp ? kCacheMinExp : e > kCacheMaxExp ? kCacheMaxExp : e;
+}
+
+// One page and head of K (V_TILES false) or V.  x: the head's elements in the row of the first token; `n` tokens from place
+// `old` on; codes: the page's codes of the head.
+template <typename T, int HS, bool V_TILES>
+struct Page {
+  // K: 16 bytes and up of a row to a lane; V: two columns to a lane, of 16 tokens (hs 128) or 8 (hs 64)
+  static constexpr int kPer = V_TILES ? 2 : 8, kLanesPerRow = HS / kPer, kGroups = 64 / kLanesPerRow, kTokens = 16 / kGroups;
+  const T* x;
+  int64_t stride;
+  uint8_t* codes;
+  int lane, old, n;
+
+  __device__ int place(int tile, int i) const {      // of a lane's i-th token
+    const int group = lane / kLanesPerRow;
+    return tile * 16 + (V_TILES ? group * kTokens + i : i * kGroups + group);
+  }
+  __device__ bool given(int p) const { return p >= old && p < old + n; }
+  __device__ int column() const { return lane % kLanesPerRow * kPer; }
+
+  __device__ void load(int tile, float (&v)[kTokens][kPer]) const {
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      const int p = place(tile, i);
+      const T* const from = x + (int64_t)(p - old) * stride + column();
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) v[i][j] = 0.0f;
+      if (given(p)) {
+        if constexpr (V_TILES) {
+          const f32x2 y = load2(from);
+          v[i][0] = y[0];
+          v[i][1] = y[1];
+        } else {
+          const f32x8 y = load8(from);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) v[i][j] = y[j];
+        }
+      }
+    }
+  }
+
+  __device__ static float most(const float (&v)[kTokens][kPer]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) m = fmaxf(m, magnitude_of(v[i][j]));
+    return m;
+  }
+
+  // `by`: what codes of older tokens are multiplied by (1: nothing)
+  __device__ void store(int tile, const float (&v)[kTokens][kPer], float inv, float by) const {
+    if constexpr (!V_TILES) {
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i) {
+        const int p = place(tile, i);
+        if (!given(p)) continue;
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = scaled(v[i][j], inv);
+        *(u32x2*)(codes + (int64_t)p * HS + column()) = u32x2{codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7])};
+      }
+    } else {
+      const int first = place(tile, 0);
+      const bool all = first >= old && first + kTokens <= old + n, none = first + kTokens <= old || first >= old + n;
+      // (a group of lanes none of whose tokens are given still has older ones to round again)
+      if (none && (by == 1.0f || first >= old)) return;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t* const at = (uint32_t*)(codes + (int64_t)tile * 16 * HS + (column() + j) * 16 + first % 16);
+        uint32_t c[kTokens / 4];
+        if constexpr (kTokens == 16) {
+          const u32x4 was = all ? u32x4{0, 0, 0, 0} : *(const u32x4*)at;
+          for (int w = 0; w < 4; ++w) c[w] = was[w];
+        } else {
+          const u32x2 was = all ? u32x2{0, 0} : *(const u32x2*)at;
+          for (int w = 0; w < 2; ++w) c[w] = was[w];
+        }
+#pragma unroll
+        for (int w = 0; w < kTokens / 4; ++w) {
+          uint32_t keep = 0, older = 0;                 // bytes that stay; bytes of older tokens
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const int p = first + 4 * w + b;
+            if (!given(p)) keep |= 0xffu << (8 * b);
+            if (p < old) older |= 0xffu << (8 * b);
+          }
+          const uint32_t fresh = codes4(scaled(v[4 * w][j], inv), scaled(v[4 * w + 1][j], inv), scaled(v[4 * w + 2][j], inv),
+                                        scaled(v[4 * w + 3][j], inv));
+          uint32_t was = c[w];
+          if (by != 1.0f) was = (recoded(was, by) & older) | (was & ~older);
+          c[w] = (fresh & ~keep) | (was & keep);
+        }
+        if constexpr (kTokens == 16) *(u32x4*)at = u32x4{c[0], c[1], c[2], c[3]};
+        else *(u32x2*)at = u32x2{c[0], c[1]};
+      }
+    }
+  }
+
+  __device__ void write(uint8_t* scale) const {
+    const int t0 = old / 16, t1 = (old + n - 1) / 16;
+    const int was = old ? (int)*scale - 127 : kCacheMinExp;
+    float v[kTokens][kPer];
+    load(t0, v);
+    float m = most(v);
+    for (int t = t0 + 1; t <= t1; ++t) {
+      float w[kTokens][kPer];
+      load(t, w);
+      m = fmaxf(m, most(w));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    int e = exponent_for(m);
+    const int floor = was < kCacheMinExp ? kCacheMinExp : was > kCacheMaxExp ? kCacheMaxExp : was;
+    e = old && floor > e ? floor : e;
+    const float inv = power_of_two(-e);
+    const int less = floor - e;
+    const float by = old && less < 0 ? power_of_two(less < -126 ? -126 : less) : 1.0f;
+    if (by != 1.0f) {      // older tokens: rows of K, whole tiles of V (the tile that the first new token shares comes below)
+      const int chunks = (V_TILES ? t0 * 16 : old) * HS / 16;
+      for (int i = lane; i < chunks; i += 64) ((u32x4*)codes)[i] = recoded(((u32x4*)codes)[i], by);
+    }
+    store(t0, v, inv, by);
+    for (int t = t0 + 1; t <= t1; ++t) {
+      load(t, v);
+      store(t, v, inv, 1.0f);
+    }
+    if (lane == 0) *scale = (uint8_t)(e + 127);
+  }
+};
+
+template <typename T, int HS>
+__global__ __launch_bounds__(kThreads) void cache_append_kernel(CacheAppendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int tensor = (int)(item & 1);
+  const int64_t rest = item >> 1, win = rest / a.hk;
+  const int head = (int)(rest - win * a.hk), page = 1 << a.page_shift;
+  const int64_t row0 = (a.first_window + win) * a.window;
+  if (win >= a.windows || row0 >= a.rows) return;
+  const auto number_of = [&](int slot) { return slot >= 0 && slot < a.slots_end ? slot >> a.page_shift : -1; };
+  bool leads = false;
+  if (lane < a.window && row0 + lane < a.rows) {
+    const int number = number_of(a.slots[row0 + lane]);
+    leads = number >= 0 && (row0 + lane == 0 || number != number_of(a.slots[row0 + lane - 1]));
+  }
+  for (uint64_t left = __ballot(leads); left; left &= left - 1) {
+    int64_t row = row0 + __builtin_ctzll(left);
+    int slot = a.slots[row];
+    const int number = slot >> a.page_shift;
+    const int64_t place = (int64_t)number * a.hk + head;
+    for (bool again = false;; again = true) {        // stretches of ascending places within the page, mostly one
+      int n = 0;
+      const int old = slot & (page - 1);
+      for (;;) {
+        const int i = n + lane;
+        const bool follows = old + i < page && row + i < a.rows && a.slots[row + i] == slot + i;
+        const uint64_t ends = ~__ballot(follows);
+        if (ends) {
+          n += __builtin_ctzll(ends);
+          break;
+        }
+        n += 64;
+      }
+      if (again) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // the stretch before wrote to this page
+      const T* const x = (const T*)a.x[tensor] + row * a.stride[tensor] + head * HS;
+      uint8_t* const codes = a.codes[tensor] + place * page * HS;
+      if (tensor) Page<T, HS, true>{x, a.stride[1], codes, lane, old, n}.write(a.scale[1] + place);
+      else Page<T, HS, false>{x, a.stride[0], codes, lane, old, n}.write(a.scale[0] + place);
+      row += n;
+      if (row >= a.rows) break;
+      slot = a.slots[row];
+      if (number_of(slot) != number) break;
+    }
+  }
+}
+
+}  // namespace
+
+int launch_cache_append(const CacheAppendArgs& args, int dtype, hipStream_t stream) {
+  CacheAppendArgs a = args;
+  // Rows in which a wave looks for pages that begin there.
+  a.window = a.rows <= 2048 ? 1 : 8;
+  // (several launches where one would have 2^32 threads or more)
+  const int64_t windows = (a.rows + a.window - 1) / a.window, most = max_workgroups(kThreads) * (kThreads / 64) / (2 * a.hk);
+  for (a.first_window = 0; a.first_window < windows; a.first_window += most) {
+    const int64_t w = a.windows = windows - a.first_window < most ? windows - a.first_window : most;
+    const dim3 g((unsigned)((w * a.hk * 2 + kThreads / 64 - 1) / (kThreads / 64)));
+    if (dtype == USP_BF16) {
+      if (a.hs == 128) cache_append_kernel<__bf16, 128><<<g, kThreads, 0, stream>>>(a);
+      else cache_append_kernel<__bf16, 64><<<g, kThreads, 0, stream>>>(a);
+    } else {
+      if (a.hs == 128) cache_append_kernel<float, 128><<<g, kThreads, 0, stream>>>(a);
+      else cache_append_kernel<float, 64><<<g, kThreads, 0, stream>>>(a);
+    }
+  }
+  return launch_status();
+}
+
+}  // namespace usp

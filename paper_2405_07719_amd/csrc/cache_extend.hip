@@ -1,0 +1,123 @@
+// Block tables, slots and positions for the tokens of a step, from request lengths that stand on the device.
+//
+// Bound: latency (a few KB at 256 requests).  One launch: every workgroup works out where each request's new pages begin in the
+// list of free ones - a sum over the requests before it, a few thousand numbers at most - and keeps that beside cu_new in
+// LDS; then each of its threads finds the request of a row by bisection.  So no workgroup waits for another, and nothing
+// is read that another one writes: pages that a request gets in this step are taken from free_pages, not from the table.
+#include "serve_internal.h"
+
+namespace usp {
+namespace {
+
+constexpr int kThreads = 256, kTokensPerThread = 4;
+
+__global__ __launch_bounds__(kThreads) void cache_extend_kernel(CacheExtendArgs a) {
+  extern __shared__ int32_t shared[];
+  int32_t* const cu = shared;                       // [n + 1], held within 0 .. total_new
+  int32_t* const first_page = shared + a.n_seqs + 1;    // [n]: place in free_pages of the request's first new page; -1: it gets none
+  __shared__ int64_t part[kThreads / 64];
+  const int tid = threadIdx.x, n = a.n_seqs, total = (int)a.total_new;
+  const int64_t page = (int64_t)1 << a.page_shift, room = (int64_t)a.max_pages * page;
+  for (int i = tid; i <= n; i += kThreads) {
+    const int x = n ? a.cu_new[i] : 0;
+    cu[i] = x < 0 ? 0 : x > total ? total : x;
+  }
+  __syncthreads();
+  // each thread has `per` requests in a row
+  const int per = (n + kThreads - 1) / kThreads, begin = tid * per < n ? tid * per : n, end = begin + per < n ? begin + per : n;
+  const auto need_of = [&](int i, int64_t* before, bool* fits) {
+    const int64_t m = cu[i + 1] > cu[i] ? cu[i + 1] - cu[i] : 0, h = a.len_before[i];
+    *before = h;
+    *fits = h >= 0 && h + m <= room && h + m <= INT32_MAX;
+    return *fits ? ((h + m + page - 1) >> a.page_shift) - ((h + page - 1) >> a.page_shift) : (int64_t)0;
+  };
+  int64_t sum = 0, h;
+  bool fits;
+  for (int i = begin; i < end; ++i) sum += need_of(i, &h, &fits);
+  int64_t upto = sum;                               // inclusive sum over the wave, then over the waves
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int64_t x = __shfl_up(upto, d);
+    if ((tid & 63) >= d) upto += x;
+  }
+  if ((tid & 63) == 63) part[tid >> 6] = upto;
+  __syncthreads();
+  int64_t asked = 0, at = upto - sum;
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < tid >> 6) at += part[w];
+    asked += part[w];
+  }
+  int64_t used = 0;
+  for (int i = begin; i < end; ++i) {
+    const int64_t need = need_of(i, &h, &fits);
+    const bool served = fits && (need == 0 || at + need <= a.n_free);
+    first_page[i] = served ? (int32_t)(need ? at : 0) : -1;
+    if (served && need) used = at + need;
+    at += need;
+    if (blockIdx.x == 0) {
+      const int m = cu[i + 1] > cu[i] ? cu[i + 1] - cu[i] : 0;
+      a.len_after[i] = served ? (int32_t)(h + m) : (int32_t)h;
+    }
+  }
+  if (blockIdx.x == 0) {
+#pragma unroll
+    for (int d = 32; d; d /= 2) {
+      const int64_t x = __shfl_xor(used, d);
+      used = x > used ? x : used;
+    }
+    __syncthreads();                                // (part has been read)
+    if ((tid & 63) == 0) part[tid >> 6] = used;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kThreads / 64; ++w) used = part[w] > used ? part[w] : used;
+      a.taken[0] = (int32_t)used;
+      a.taken[1] = (int32_t)(asked < INT32_MAX ? asked : INT32_MAX);
+    }
+  }
+  __syncthreads();
+  for (int k = 0; k < kTokensPerThread; ++k) {
+    const int64_t t = ((int64_t)blockIdx.x * kTokensPerThread + k) * kThreads + tid;
+    if (t >= total) break;
+    int lo = 0, hi = n;                             // the last request that begins at t or before: cu[lo] <= t < cu[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (cu[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    int32_t slot = -1, pos = 0;
+    if (n && cu[lo] <= t && t < cu[lo + 1]) {
+      const int64_t had = a.len_before[lo], p = had + t - cu[lo];
+      pos = (int32_t)p;
+      if (first_page[lo] >= 0) {
+        const int64_t index = p >> a.page_shift, held = (had + page - 1) >> a.page_shift;
+        int32_t* const entry = a.block_table + (int64_t)lo * a.max_pages + index;
+        int32_t number;
+        if (index >= held) {
+          number = a.free_pages[first_page[lo] + (index - held)];
+          if ((p & (page - 1)) == 0) *entry = number;     // the first row of a new page is one of this step
+        } else {
+          number = *entry;
+        }
+        if (number >= 0 && number < a.pages) slot = (int32_t)(((int64_t)number << a.page_shift) + (p & (page - 1)));
+      }
+    }
+    a.slots[t] = slot;
+    a.positions[t] = pos;
+  }
+}
+
+}  // namespace
+
+int launch_cache_extend(const CacheExtendArgs& a, hipStream_t stream) {
+  const size_t lds = (size_t)(2 * a.n_seqs + 1) * sizeof(int32_t);      // 64 KiB and 4 bytes at most
+  if (lds > 48 * 1024) {
+    static LdsLimitRaised raised;
+    if (!raise_dynamic_lds_limit((const void*)cache_extend_kernel, 80 * 1024, raised)) return USP_ERR_LAUNCH;
+  }
+  int64_t grid = (a.total_new + kThreads * kTokensPerThread - 1) / (kThreads * kTokensPerThread);
+  if (grid < 1) grid = 1;
+  cache_extend_kernel<<<dim3((unsigned)grid), kThreads, lds, stream>>>(a);
+  return launch_status();
+}
+
+}  // namespace usp
