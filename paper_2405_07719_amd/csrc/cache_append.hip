@@ -18,20 +18,8 @@ namespace {
 constexpr int kThreads = 256;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-__device__ inline f32x8 load8(const __bf16* p) { return __builtin_convertvector(*(const bf16x8*)p, f32x8); }
-__device__ inline f32x8 load8(const float* p) {
-  const f32x4 a = ((const f32x4*)p)[0], b = ((const f32x4*)p)[1];
-  return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-}
-__device__ inline f32x2 load2(const __bf16* p) { return __builtin_convertvector(*(const bf16x2*)p, f32x2); }
-__device__ inline f32x2 load2(const float* p) { return *(const f32x2*)p; }
 
 __device__ inline float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
 
@@ -41,8 +29,8 @@ __device__ inline float magnitude_of(float x) {
   return y <= FLT_MAX ? y : 0.0f;
 }
 
-// x / 2^e as the conversion takes it: NaN for NaN and infinities, at most the largest code
-__device__ inline float scaled(float x, float inv) {
+// x / 2^e as the conversion takes it where values may be infinite or beyond the largest code: NaN for NaN and infinities
+__device__ inline float held(float x, float inv) {
   const float y = x * inv, z = fabsf(y) > 448.0f ? copysignf(448.0f, y) : y;
   return fabsf(x) <= FLT_MAX ? z : __int_as_float(0x7fc00000);
 }
@@ -68,12 +56,27 @@ __device__ inline int exponent_for(float most) {
   return e < kCacheMinExp ? kCacheMinExp : e > kCacheMaxExp ? kCacheMaxExp : e;
 }
 
+// Two neighbouring elements as they were loaded, and as numbers.
+template <typename T> struct Two;
+template <> struct Two<__bf16> {
+  typedef uint32_t raw;
+  static __device__ f32x2 values(raw x) { return f32x2{__int_as_float((int)(x << 16)), __int_as_float((int)(x & 0xffff0000u))}; }
+};
+template <> struct Two<float> {
+  typedef u32x2 raw;
+  static __device__ f32x2 values(raw x) { return f32x2{__int_as_float((int)x[0]), __int_as_float((int)x[1])}; }
+};
+
 // One page and head of K (V_TILES false) or V.  x: the head's elements in the row of the first token; `n` tokens from place
 // `old` on; codes: the page's codes of the head.
 template <typename T, int HS, bool V_TILES>
 struct Page {
-  // K: 16 bytes and up of a row to a lane; V: two columns to a lane, of 16 tokens (hs 128) or 8 (hs 64)
-  static constexpr int kPer = V_TILES ? 2 : 8, kLanesPerRow = HS / kPer, kGroups = 64 / kLanesPerRow, kTokens = 16 / kGroups;
+  // K: eight elements of a row to a lane; V: two columns to a lane, of 16 tokens (hs 128) or 8 (hs 64)
+  static constexpr int kPer = V_TILES ? 2 : 8, kPairs = kPer / 2, kLanesPerRow = HS / kPer, kGroups = 64 / kLanesPerRow,
+                       kTokens = 16 / kGroups;
+  // Tiles whose values are all on their way, and stay in registers, at once: the 64 tokens of an ordinary page.
+  static constexpr int kTiles = 4;
+  typedef typename Two<T>::raw Raw;
   const T* x;
   int64_t stride;
   uint8_t* codes;
@@ -86,64 +89,83 @@ struct Page {
   __device__ bool given(int p) const { return p >= old && p < old + n; }
   __device__ int column() const { return lane % kLanesPerRow * kPer; }
 
-  __device__ void load(int tile, float (&v)[kTokens][kPer]) const {
+  // A lane's elements of a tile.  Places that are not given read one that is: a load under a condition would be waited for
+  // where it stands, one after the other.
+  __device__ void load(int tile, Raw (&v)[kTokens][kPairs]) const {
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
-      const int p = place(tile, i);
-      const T* const from = x + (int64_t)(p - old) * stride + column();
+      int p = place(tile, i) - old;
+      p = p < 0 ? 0 : p < n ? p : n - 1;
+      const T* const from = x + p * stride + column();
+      if constexpr (V_TILES) {
+        v[i][0] = *(const Raw*)from;
+      } else {
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) v[i][j] = 0.0f;
-      if (given(p)) {
-        if constexpr (V_TILES) {
-          const f32x2 y = load2(from);
-          v[i][0] = y[0];
-          v[i][1] = y[1];
-        } else {
-          const f32x8 y = load8(from);
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) v[i][j] = y[j];
-        }
+        for (int w = 0; w < (int)sizeof(T) / 2; ++w) ((u32x4*)v[i])[w] = ((const u32x4*)from)[w];
       }
     }
   }
 
-  __device__ static float most(const float (&v)[kTokens][kPer]) {
+  // largest magnitude, infinity among them (a place that is not given repeats one that is)
+  __device__ static float most(const Raw (&v)[kTokens][kPairs]) {
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < kTokens; ++i)
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) m = fmaxf(m, magnitude_of(v[i][j]));
+      for (int j = 0; j < kPairs; ++j) {
+        const f32x2 y = Two<T>::values(v[i][j]);
+        m = fmaxf(m, fmaxf(fabsf(y[0]), fabsf(y[1])));
+      }
+    return m;
+  }
+  __device__ static float most_finite(const Raw (&v)[kTokens][kPairs]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i)
+#pragma unroll
+      for (int j = 0; j < kPairs; ++j) {
+        const f32x2 y = Two<T>::values(v[i][j]);
+        m = fmaxf(m, fmaxf(magnitude_of(y[0]), magnitude_of(y[1])));
+      }
     return m;
   }
 
-  // `by`: what codes of older tokens are multiplied by (1: nothing)
-  __device__ void store(int tile, const float (&v)[kTokens][kPer], float inv, float by) const {
+  // `odd`: infinities or values beyond the largest code may be among them; `by`: what codes of older tokens are multiplied
+  // by (1: nothing)
+  __device__ void store(int tile, const Raw (&v)[kTokens][kPairs], float inv, bool odd, float by) const {
+    const auto code = [&](float y) { return odd ? held(y, inv) : y * inv; };
     if constexpr (!V_TILES) {
 #pragma unroll
       for (int i = 0; i < kTokens; ++i) {
         const int p = place(tile, i);
-        if (!given(p)) continue;
-        float y[8];
+        f32x2 y[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = scaled(v[i][j], inv);
-        *(u32x2*)(codes + (int64_t)p * HS + column()) = u32x2{codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7])};
+        for (int j = 0; j < 4; ++j) {
+          y[j] = Two<T>::values(v[i][j]);
+          y[j] = f32x2{code(y[j][0]), code(y[j][1])};
+        }
+        if (given(p))
+          *(u32x2*)(codes + p * HS + column()) = u32x2{codes4(y[0][0], y[0][1], y[1][0], y[1][1]), codes4(y[2][0], y[2][1], y[3][0], y[3][1])};
       }
     } else {
       const int first = place(tile, 0);
       const bool all = first >= old && first + kTokens <= old + n, none = first + kTokens <= old || first >= old + n;
       // (a group of lanes none of whose tokens are given still has older ones to round again)
       if (none && (by == 1.0f || first >= old)) return;
+      uint32_t c[2][kTokens / 4];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t* const at = (uint32_t*)(codes + (int64_t)tile * 16 * HS + (column() + j) * 16 + first % 16);
-        uint32_t c[kTokens / 4];
-        if constexpr (kTokens == 16) {
-          const u32x4 was = all ? u32x4{0, 0, 0, 0} : *(const u32x4*)at;
-          for (int w = 0; w < 4; ++w) c[w] = was[w];
-        } else {
-          const u32x2 was = all ? u32x2{0, 0} : *(const u32x2*)at;
-          for (int w = 0; w < 2; ++w) c[w] = was[w];
+      for (int w = 0; w < kTokens / 4; ++w) {
+        f32x2 y[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          y[b] = Two<T>::values(v[4 * w + b][0]);
+          y[b] = f32x2{code(y[b][0]), code(y[b][1])};
         }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) c[j][w] = codes4(y[0][j], y[1][j], y[2][j], y[3][j]);
+      }
+      uint32_t* const at = (uint32_t*)(codes + tile * 16 * HS + column() * 16 + first % 16);
+      if (!all) {
 #pragma unroll
         for (int w = 0; w < kTokens / 4; ++w) {
           uint32_t keep = 0, older = 0;                 // bytes that stay; bytes of older tokens
@@ -153,45 +175,75 @@ struct Page {
             if (!given(p)) keep |= 0xffu << (8 * b);
             if (p < old) older |= 0xffu << (8 * b);
           }
-          const uint32_t fresh = codes4(scaled(v[4 * w][j], inv), scaled(v[4 * w + 1][j], inv), scaled(v[4 * w + 2][j], inv),
-                                        scaled(v[4 * w + 3][j], inv));
-          uint32_t was = c[w];
-          if (by != 1.0f) was = (recoded(was, by) & older) | (was & ~older);
-          c[w] = (fresh & ~keep) | (was & keep);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t was = at[4 * j + w];
+            if (by != 1.0f) was = (recoded(was, by) & older) | (was & ~older);
+            c[j][w] = (c[j][w] & ~keep) | (was & keep);
+          }
         }
-        if constexpr (kTokens == 16) *(u32x4*)at = u32x4{c[0], c[1], c[2], c[3]};
-        else *(u32x2*)at = u32x2{c[0], c[1]};
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if constexpr (kTokens == 16) *(u32x4*)(at + 4 * j) = u32x4{c[j][0], c[j][1], c[j][2], c[j][3]};
+        else *(u32x2*)(at + 4 * j) = u32x2{c[j][0], c[j][1]};
       }
     }
   }
 
   __device__ void write(uint8_t* scale) const {
-    const int t0 = old / 16, t1 = (old + n - 1) / 16;
+    const int t0 = old / 16, tiles = (old + n - 1) / 16 - t0 + 1;
     const int was = old ? (int)*scale - 127 : kCacheMinExp;
-    float v[kTokens][kPer];
-    load(t0, v);
-    float m = most(v);
-    for (int t = t0 + 1; t <= t1; ++t) {
-      float w[kTokens][kPer];
-      load(t, w);
-      m = fmaxf(m, most(w));
-    }
+    Raw v[kTiles][kTokens][kPairs];
+    // the first tiles last, so that they are in registers when their codes are formed
+    float m = 0.0f, finite = 0.0f;
+    bool infinite = false;
+    for (int round = 0; round < 2; ++round) {
+      for (int t = tiles > kTiles ? kTiles : 0; ; t = 0) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+        for (int i = 0; i < kTiles; ++i)
+          if (t + i < tiles && (round == 0 || tiles > kTiles)) load(t0 + t + i, v[i]);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+          if (t + i < tiles) {
+            if (round == 0) m = fmaxf(m, most(v[i]));
+            else finite = fmaxf(finite, most_finite(v[i]));
+          }
+        if (t == 0) break;
+      }
+      if (round == 0) {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+        infinite = m > FLT_MAX;
+        if (!infinite) break;
+      }
+    }
+    if (infinite) {
+      m = finite;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    }
     int e = exponent_for(m);
     const int floor = was < kCacheMinExp ? kCacheMinExp : was > kCacheMaxExp ? kCacheMaxExp : was;
     e = old && floor > e ? floor : e;
     const float inv = power_of_two(-e);
+    const bool odd = infinite || m * inv > 448.0f;
     const int less = floor - e;
     const float by = old && less < 0 ? power_of_two(less < -126 ? -126 : less) : 1.0f;
     if (by != 1.0f) {      // older tokens: rows of K, whole tiles of V (the tile that the first new token shares comes below)
       const int chunks = (V_TILES ? t0 * 16 : old) * HS / 16;
       for (int i = lane; i < chunks; i += 64) ((u32x4*)codes)[i] = recoded(((u32x4*)codes)[i], by);
     }
-    store(t0, v, inv, by);
-    for (int t = t0 + 1; t <= t1; ++t) {
-      load(t, v);
-      store(t, v, inv, 1.0f);
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+      if (i < tiles) store(t0 + i, v[i], inv, odd, by);
+    if (tiles > kTiles) {
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+        if (kTiles + i < tiles) load(t0 + kTiles + i, v[i]);
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+        if (kTiles + i < tiles) store(t0 + kTiles + i, v[i], inv, odd, 1.0f);
     }
     if (lane == 0) *scale = (uint8_t)(e + 127);
   }

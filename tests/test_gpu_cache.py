@@ -74,7 +74,9 @@ def append_case(usp, page, hk, hs, dtype, olds, news, seed, strided=False, sprea
     k, v = (torch.from_numpy(rng.standard_normal((rows, hk, hs)) * size).to(t).cuda() for _ in range(2))
     if special:
         for x in (k, v):
-            x[0, 0, 0], x[rows // 2, hk - 1, hs - 1], x[rows - 1, 0, 3] = float("nan"), float("inf"), float("-inf")
+            x[0, 0, 0] = x[rows - 1, 1, 2] = float("nan")
+            if special == "infinite":
+                x[rows // 2, hk - 1, hs - 1], x[rows - 1, 0, 3] = float("inf"), float("-inf")
             x[rows // 3] = 0.0
     if strided:
         both = torch.zeros(rows, 3 * hk, hs, dtype=t, device="cuda")
@@ -113,7 +115,9 @@ def test_append_of_many_rows(usp, rows):
 
 @pytest.mark.parametrize("dtype", [sl.BF16, sl.FP32])
 def test_append_of_nan_infinity_and_zero(usp, dtype):
-    append_case(usp, 32, 2, 128, dtype, [3, 0, 0], [4, 50, 1], 5, special=True)
+    for special in ("nan", "infinite"):
+        append_case(usp, 32, 2, 128, dtype, [3, 0, 0], [4, 50, 1], 5, special=special)
+        append_case(usp, 128, 2, 64, dtype, [0, 60], [128, 10], 6, special=special)
 
 
 def test_exponents_at_their_ends(usp):
