@@ -403,8 +403,8 @@ int usp_cache_extend(const int32_t* cu_new, const int32_t* len_before, int n_seq
 
 /* Writes K and V of `rows` tokens to their slots.  k, v: rows of hk heads of hs elements side by side, k_stride and v_stride
  * elements apart (bf16 or fp32).  slots [rows]; a slot outside [0, pages * page) is skipped.
- *   Per page, head and tensor, the exponent is the smallest with which every value lies within 448 * 2^e (within [-117, 96];
- *   values beyond 448 * 2^96 are held at the largest code), at least what the page has already if tokens stand before the first
+ *   Per page, head and tensor, the exponent is the smallest with which every value lies within 448 * 2^e (within [-117, 88];
+ *   values beyond 448 * 2^88 are held at the largest code), at least what the page has already if tokens stand before the first
  *   one written; where it grows, their codes are rounded again to the new exponent.  Writing place 0 starts a page anew.
  *   Values are rounded to the nearest code, ties to even; NaN and infinities are held as NaN and do not count for e.
  * Rows of one page have to stand together in `slots` (as usp_cache_extend gives them); stretches of ascending places are

@@ -10,7 +10,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libusp.so")
 SOURCES = ["usp_api.cpp", "layout_a2a.hip", "lse_merge.hip", "block_attn_fwd.hip", "wave_split_attn_fwd.hip",
-           "block_attn_bwd.hip", "serve_api.cpp", "rope.hip", "cache_extend.hip", "cache_append.hip", "cache_attn.hip"]
+           "block_attn_bwd.hip", "serve_api.cpp", "rope.hip", "cache_extend.hip", "cache_append.hip", "cache_attn.hip",
+           "cache_attn_rows.hip"]
 # measurement aid for bench.py only (matrix-core calibration loops): a library of its own, not part of the product
 CALIB_LIB = os.path.join(PKG, "libusp_calib.so")
 CALIB_SOURCES = ["calib_mfma.hip"]

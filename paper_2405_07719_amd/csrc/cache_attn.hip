@@ -12,34 +12,13 @@
 // all along: row c = lane % 16, keys and elements by g = lane / 16.  Row 4 g' + r of the t-th 16-key product of a step
 // is key 16 g' + 4 t + r, which gives lane group g the 16 keys of one block of the cache: its P is, as it stands, the
 // operand of the second product, whose V operand is 16 bytes of one column of a V tile.  Nothing goes through LDS.
-#include <math.h>
-
-#include "serve_internal.h"
+#include "cache_attn_device.h"
 
 namespace usp {
 namespace {
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kThreads = 256, kStep = kCacheStep;
 typedef CacheUnits Units;
-
-// What a wave leaves for the joining launch: `first`: 0, or its share begins inside a unit, which goes on behind it (1) or
-// ends in it (2); seq >= 0: its share ends inside the unit (seq, head, tile), which begins in it.
-struct Left { int first, seq, head, tile; };
-
-struct Plan {
-  CacheAttnArgs a;
-  int waves;          // that have a share, at most; places in `left`
-  Left* left;
-  float* partial;     // [waves][2][RT][hs + 2]: per row m, l, then O
-  int rows_per_tile;
-};
 
 __device__ inline float group_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -50,65 +29,44 @@ __device__ inline float group_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// eight codes as the operand of a product
-__device__ inline bf16x8 widened(uint32_t lo, uint32_t hi, float scale) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// 0x80 in each byte that is a NaN code
-__device__ inline uint32_t nan_codes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-
-// bytes of a word whose first `n` (any number) stay
-__device__ inline uint32_t first_bytes(int n) { return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : 0xffffffffu >> (32 - 8 * n); }
-
 template <int HS, int R>
 struct Walk {
   static constexpr int RT = 16 * R, KI = HS / 32, ET = HS / 16, KV16 = HS / 64;     // KV16: 16-byte reads of a K row's quarter
-  const Plan& p;
+  const CachePlan& p;
   int lane, c, g;
 
   // a step's codes and scales
   u32x4 k[4][KV16], v[ET];
-  float ks, vs;
+  uint32_t ks, vs;
   int number_k, number_v;       // pages of the blocks that the lane reads of K and of V; -1: none
 
-  __device__ explicit Walk(const Plan& plan, int l) : p(plan), lane(l), c(l & 15), g(l >> 4) {}
+  __device__ explicit Walk(const CachePlan& plan, int l) : p(plan), lane(l), c(l & 15), g(l >> 4) {}
 
+  // (Neither lookups nor loads stand under a condition, where each would be waited for before the next: a block behind the last
+  // one that counts is looked up as that one, and a page that is not there reads page 0.)
   __device__ void find(const int32_t* row, int step, int vis) {
-    number_k = cache_page(p.a, row, step * 4 + (c >> 2), vis);
-    number_v = cache_page(p.a, row, step * 4 + g, vis);
+    const int bk = step * 4 + (c >> 2), bv = step * 4 + g;
+    const int nk = row[cache_entry(bk, vis, p.a.page_shift)], nv = row[cache_entry(bv, vis, p.a.page_shift)];
+    number_k = cache_counts(bk, vis, nk, p.a.pages) ? nk : -1;
+    number_v = cache_counts(bv, vis, nv, p.a.pages) ? nv : -1;
   }
   __device__ void load_k(int step, int head) {
     const int inside = ((step * 4 + (c >> 2)) * 16) & ((1 << p.a.page_shift) - 1);
-    const int64_t place = (int64_t)number_k * p.a.hk + head;
+    const int64_t place = (int64_t)(number_k < 0 ? 0 : number_k) * p.a.hk + head;
     const uint8_t* const at = p.a.k_codes + ((place << p.a.page_shift) + inside + (c & 3)) * HS + g * (HS / 4);
-    ks = 1.0f;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int i = 0; i < KV16; ++i) k[t][i] = u32x4{0, 0, 0, 0};
-    if (number_k >= 0) {
-      ks = __int_as_float((int)p.a.k_scale[place] << 23);
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < KV16; ++i) k[t][i] = *(const u32x4*)(at + t * 4 * HS + i * 16);
-    }
+      for (int i = 0; i < KV16; ++i) k[t][i] = *(const u32x4*)(at + t * 4 * HS + i * 16);
+    ks = p.a.k_scale[place];
   }
   __device__ void load_v(int step, int head) {
     const int inside = ((step * 4 + g) * 16) & ((1 << p.a.page_shift) - 1);
-    const int64_t place = (int64_t)number_v * p.a.hk + head;
+    const int64_t place = (int64_t)(number_v < 0 ? 0 : number_v) * p.a.hk + head;
     const uint8_t* const at = p.a.v_codes + ((place << p.a.page_shift) + inside) * HS + c * 16;
-    vs = 1.0f;
 #pragma unroll
-    for (int e = 0; e < ET; ++e) v[e] = u32x4{0, 0, 0, 0};
-    if (number_v >= 0) {
-      vs = __int_as_float((int)p.a.v_scale[place] << 23);
-#pragma unroll
-      for (int e = 0; e < ET; ++e) v[e] = *(const u32x4*)(at + e * 256);
-    }
+    for (int e = 0; e < ET; ++e) v[e] = *(const u32x4*)(at + e * 256);
+    vs = p.a.v_scale[place];
   }
 
   // Steps [s0, s1) of a unit of `steps` ones: results to o and lse if these are all, else to partial result `slot`.
@@ -146,6 +104,7 @@ struct Walk {
       const bool more = s + 1 < end;
       const bool valid = number_v >= 0;               // of the block whose 16 keys the lane's scores are
       if (more) find(row, s + 1, vis);
+      const float scale_k = scale_of(ks);
       // S^T = K Q^T
       f32x4 x[R][4];
 #pragma unroll
@@ -154,14 +113,14 @@ struct Walk {
         for (int r = 0; r < R; ++r) x[r][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
-          const bf16x8 w = widened(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1], ks);
+          const bf16x8 w = widened(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1], scale_k);
 #pragma unroll
           for (int r = 0; r < R; ++r) x[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, q[r][i], x[r][t], 0, 0, 0);
         }
       }
       if (more) load_k(s + 1, head);
       const int key0 = s * kStep + g * 16;            // the lane's first key
-      const bool masked = (s + 1) * kStep > vis_first || __ballot(!valid);
+      const bool missing = __ballot(!valid) != 0, masked = (s + 1) * kStep > vis_first || missing;
       if (masked) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -201,12 +160,15 @@ struct Walk {
 #pragma unroll
           for (int e = 0; e < 8; ++e) pr[r][j][e] = (__bf16)x[r][2 * j + e / 4][e % 4];
       }
-      // what stands behind the last key counts as zero, whatever it is
-      if ((s + 1) * kStep > vis) {
+      // what stands behind the last key, or in a page that is not there, counts as zero, whatever it is
+      if ((s + 1) * kStep > vis || missing) {
+        const int left = valid ? vis - key0 : 0;
 #pragma unroll
-        for (int e = 0; e < ET; ++e)
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t stay = first_bytes(left - 4 * w);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) v[e][w] &= first_bytes(vis - key0 - 4 * w);
+          for (int e = 0; e < ET; ++e) v[e][w] &= stay;
+        }
       }
       // NaN in a value that some rows of the tile see and others do not: 0 times it would be NaN for those.  Counted apart,
       // with another product, and taken as zero in the one that counts.
@@ -245,11 +207,12 @@ struct Walk {
         }
       }
       // O^T += V^T P^T
+      const float scale_v = valid ? scale_of(vs) : 1.0f;      // (0 times the NaN of a page in no use would be NaN)
 #pragma unroll
       for (int e = 0; e < ET; ++e)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const bf16x8 w = widened(v[e][2 * j], v[e][2 * j + 1], vs);
+          const bf16x8 w = widened(v[e][2 * j], v[e][2 * j + 1], scale_v);
 #pragma unroll
           for (int r = 0; r < R; ++r) o[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, pr[r][j], o[r][e], 0, 0, 0);
         }
@@ -270,7 +233,7 @@ struct Walk {
           if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to + e * 16) = __builtin_convertvector(y, bf16x4);
           else *(f32x4*)((float*)a.o + to + e * 16) = y;
         }
-        if (g == 0) a.lse[(int64_t)h * a.total_q + u.cu + token] = l[r] == 0.0f ? -INFINITY : (m[r] + log2f(l[r])) * 0.693147180559945309f;
+        if (g == 0) a.lse[(int64_t)h * a.total_q + u.cu + token] = natural_lse(m[r], l[r]);
       } else {
         float* const to = slot + (int64_t)at * (HS + 2);
         if (g == 0) *(f32x2*)to = f32x2{m[r], l[r]};
@@ -285,88 +248,46 @@ struct Walk {
 };
 
 template <int HS, int R>
-__global__ __launch_bounds__(kThreads, R == 4 ? 1 : 2) void cache_attn_kernel(Plan p) {
-  __shared__ int64_t before[kThreads + 1];       // steps of the requests before a thread's first one
-  __shared__ int64_t part[kThreads / 64];
-  const CacheAttnArgs& a = p.a;
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
+  __shared__ Shares<kThreads> shares;
   constexpr int RT = 16 * R;
-  const int tid = threadIdx.x, lane = tid & 63, n = a.n_seqs;
-  const int per = (n + kThreads - 1) / kThreads;
-  int64_t sum = 0;
-  for (int i = tid * per; i < (tid + 1) * per && i < n; ++i) sum += Units(a, i, RT).per_head * a.hk;
-  int64_t upto = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t x = __shfl_up(upto, d);
-    if (lane >= d) upto += x;
-  }
-  if (lane == 63) part[tid >> 6] = upto;
-  __syncthreads();
-  int64_t all = 0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < tid >> 6) upto += part[w];
-    all += part[w];
-  }
-  before[tid + 1] = upto;
-  if (tid == 0) before[0] = 0;
-  __syncthreads();
-
-  const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) * (int)gridDim.x + (int)blockIdx.x);
-  const int shares = all < p.waves ? (int)all : p.waves;
-  Left left = {0, -1, 0, 0};
-  if (wave < shares) {
-    int64_t pos = all * wave / shares;
-    const int64_t stop = all * (wave + 1) / shares;
+  const int64_t all = shares.count(p.a, RT);
+  const int wave = __builtin_amdgcn_readfirstlane(((int)threadIdx.x >> 6) * (int)gridDim.x + (int)blockIdx.x);
+  const int workers = all < p.workers ? (int)all : p.workers;
+  CacheLeft left = {0, -1, 0, 0};
+  if (wave < workers) {
+    Walk<HS, R> walk(p, threadIdx.x & 63);
     float* const slots = p.partial + (int64_t)wave * 2 * RT * (HS + 2);
-    int lo = 0, hi = kThreads;                   // the last thread whose first request begins at pos or before
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (before[mid] <= pos) lo = mid;
-      else hi = mid;
-    }
-    int64_t start = before[lo];                  // where request `seq` begins
-    int seq = __builtin_amdgcn_readfirstlane(lo * per);
-    Walk<HS, R> walk(p, lane);
-    while (pos < stop && seq < n) {
-      const Units u(a, seq, RT);
-      const int64_t steps = u.per_head * a.hk;
-      if (pos >= start + steps) {
-        start += steps;
-        ++seq;
-        continue;
-      }
-      const CacheUnits::Place at = u.locate(pos - start);
-      const int head = at.head, tile = at.tile, s0 = at.step, of = u.steps(tile);
-      const int s1 = stop - pos < of - s0 ? s0 + (int)(stop - pos) : of;
-      const bool begins = s0 == 0, ends = s1 == of;
-      walk.unit(u, seq, head, tile, s0, s1, begins && ends, slots + (begins ? RT * (HS + 2) : 0));
-      if (!begins) left.first = ends ? 2 : 1;
-      else if (!ends) left.seq = seq, left.head = head, left.tile = tile;
-      pos += s1 - s0;
-    }
+    shares.walk(p.a, RT, all * wave / workers, all * (wave + 1) / workers,
+                [&](const CacheUnits& u, int seq, const CacheUnits::Place& at, int end, int of) __attribute__((always_inline)) {
+                  const bool begins = at.step == 0, ends = end == of;
+                  walk.unit(u, seq, at.head, at.tile, at.step, end, begins && ends, slots + (begins ? RT * (HS + 2) : 0));
+                  if (!begins) left.first = ends ? 2 : 1;
+                  else if (!ends) left.seq = seq, left.head = at.head, left.tile = at.tile;
+                });
   }
-  if (lane == 0 && wave < p.waves) p.left[wave] = left;
+  if ((threadIdx.x & 63) == 0 && wave < p.workers) p.left[wave] = left;
 }
 
-// Joins the partial results of one unit: the beginning that wave w left, then what the waves behind it left up to the unit's end.
-template <int HS, int R>
-__global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(Plan p) {
-  constexpr int RT = 16 * R, kSlot = RT * (HS + 2);
+// Joins the partial results of one unit: the beginning that worker w left, then what the workers behind it left up to the unit's
+// end.  blockIdx.y: which of the unit's rows.
+template <int HS>
+__global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(CachePlan p, int rows_per_tile) {
+  const int64_t slot = (int64_t)rows_per_tile * (HS + 2);
   const CacheAttnArgs& a = p.a;
   const int w = blockIdx.x;
-  const Left mine = p.left[w];
+  const CacheLeft mine = p.left[w];
   if (mine.seq < 0) return;
-  const Units u(a, mine.seq, RT);
-  const int rows = u.rows(a, mine.tile, RT);
+  const CacheUnits u(a, mine.seq, rows_per_tile);
+  const int rows = u.rows(a, mine.tile, rows_per_tile);
   int last = w + 1;
-  while (last < p.waves - 1 && p.left[last].first == 1) ++last;
-  for (int i = threadIdx.x; i < rows * HS; i += kThreads) {
+  while (last < p.workers - 1 && p.left[last].first == 1) ++last;
+  for (int i = blockIdx.y * kThreads + threadIdx.x; i < rows * HS; i += kThreads * gridDim.y) {
     const int row = i / HS, e = i - row * HS;
-    const float* at = p.partial + (int64_t)(2 * w + 1) * kSlot + row * (HS + 2);
+    const float* at = p.partial + (2 * (int64_t)w + 1) * slot + row * (HS + 2);
     float m = at[0], l = at[1], o = at[2 + e];
     for (int x = w + 1; x <= last; ++x) {
-      at = p.partial + (int64_t)(2 * x) * kSlot + row * (HS + 2);
+      at = p.partial + 2 * (int64_t)x * slot + row * (HS + 2);
       const float mx = at[0], lx = at[1], ox = at[2 + e];
       const float top = fmaxf(m, mx), use = top == -INFINITY ? 0.0f : top;
       const float keep = exp2f(m - use), add = exp2f(mx - use);
@@ -374,48 +295,43 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(Plan p) {
       o = o * keep + ox * add;
       m = top;
     }
-    const int64_t row_in = (int64_t)mine.tile * RT + row;
+    const int64_t row_in = (int64_t)mine.tile * rows_per_tile + row;
     const int token = (int)(row_in / a.group), h = mine.head * a.group + (int)(row_in - (int64_t)token * a.group);
     const float y = l == 0.0f ? 0.0f : o / l;
     const int64_t to = ((int64_t)(u.cu + token) * (a.hk * a.group) + h) * HS + e;
     if (a.o_dtype == USP_BF16) ((__bf16*)a.o)[to] = (__bf16)y;
     else ((float*)a.o)[to] = y;
-    if (e == 0) a.lse[(int64_t)h * a.total_q + u.cu + token] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+    if (e == 0) a.lse[(int64_t)h * a.total_q + u.cu + token] = natural_lse(m, l);
   }
 }
 
-int tiles_of_16(int group, int max_q) {
-  const int64_t rows = (int64_t)group * (max_q < 1 ? 1 : max_q);
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-}
-int waves_for(int r) { return r == 4 ? kPlanCUs * 4 : kPlanCUs * 8; }
-
-template <int HS, int R>
-void launch(const Plan& p, hipStream_t stream) {
-  cache_attn_kernel<HS, R><<<dim3(p.waves / (kThreads / 64)), kThreads, 0, stream>>>(p);
-  cache_attn_join_kernel<HS, R><<<dim3(p.waves), kThreads, 0, stream>>>(p);
-}
+// Up to 16 rows of a request fit one product of the kernel that has a wave to itself; more go to the kernel for many rows.
+bool few_rows(int group, int max_q) { return (int64_t)group * (max_q < 1 ? 1 : max_q) <= 16; }
+int rows_of(bool few) { return few ? 16 : kCacheRowsTile; }
+int workers_of(bool few) { return few ? kPlanCUs * 8 : kPlanCUs; }
 
 }  // namespace
 
 size_t cache_attn_workspace(int group, int hs, int max_q) {
-  const int r = tiles_of_16(group, max_q);
-  return (size_t)waves_for(r) * (sizeof(Left) + (size_t)2 * 16 * r * (hs + 2) * sizeof(float));
+  const bool few = few_rows(group, max_q);
+  return (size_t)workers_of(few) * (sizeof(CacheLeft) + (size_t)2 * rows_of(few) * (hs + 2) * sizeof(float));
 }
 
 int launch_cache_attn(const CacheAttnArgs& a, int max_q, hipStream_t stream) {
-  const int r = tiles_of_16(a.group, max_q);
-  Plan p = {a, waves_for(r), (Left*)a.workspace, nullptr, 16 * r};
-  p.partial = (float*)(p.left + p.waves);
-  if (a.hs == 128) {
-    if (r == 1) launch<128, 1>(p, stream);
-    else if (r == 2) launch<128, 2>(p, stream);
-    else launch<128, 4>(p, stream);
+  const bool few = few_rows(a.group, max_q);
+  CachePlan p = {a, workers_of(few), (CacheLeft*)a.workspace, nullptr};
+  p.partial = (float*)(p.left + p.workers);
+  if (few) {
+    const dim3 grid(p.workers / (kThreads / 64));
+    if (a.hs == 128) cache_attn_kernel<128, 1><<<grid, kThreads, 0, stream>>>(p);
+    else cache_attn_kernel<64, 1><<<grid, kThreads, 0, stream>>>(p);
   } else {
-    if (r == 1) launch<64, 1>(p, stream);
-    else if (r == 2) launch<64, 2>(p, stream);
-    else launch<64, 4>(p, stream);
+    const int st = launch_cache_attn_rows(p, stream);
+    if (st != USP_OK) return st;
   }
+  const dim3 grid(p.workers, few ? 1 : 8);
+  if (a.hs == 128) cache_attn_join_kernel<128><<<grid, kThreads, 0, stream>>>(p, rows_of(few));
+  else cache_attn_join_kernel<64><<<grid, kThreads, 0, stream>>>(p, rows_of(few));
   return launch_status();
 }
 

@@ -1,0 +1,312 @@
+// Attention over the 8-bit cache for many rows of a request (pieces of prompts): bound by the matrix cores.
+//
+// A unit is one request, KV head and tile of 256 rows (tokens x query heads of the KV head); the steps of all units, laid one
+// behind the other, are cut evenly among one workgroup per CU, and units that are cut leave partial results for the joining
+// launch (see cache_attn.hip).  A workgroup is 8 waves of 32 rows, two to a SIMD.  Codes are widened to bf16 once per
+// workgroup, on their way into LDS, not once per wave: K as rows, V as the tiles lie, transposed, both with strides that keep
+// 16-byte reads free of bank conflicts (HS * 2 + 16 and 144 bytes: an odd number of 16-byte pieces).
+//
+// S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row (lane % 32) and every product's operand is what the one before
+// leaves: of 16 tokens of V the lanes below 32 need 0-3 and 8-11, the others 4-7 and 12-15, which is the order in which they
+// are written to LDS.
+//
+// Step s: the maxima of its scores; then, side by side, the scores of step s + 1 (matrix cores), the exponentials of step s
+// (vector ALU) and the products with V; while the codes of K two steps ahead and of V one step ahead are on their way.
+// K and V have two buffers each, and a step ends with the one barrier that they need.
+#include "cache_attn_device.h"
+
+namespace usp {
+namespace {
+
+constexpr int kThreads = 512, kStep = kCacheStep, kRows = 32;
+
+template <int HS> constexpr int k_stride() { return HS * 2 + 16; }
+constexpr int kVStride = kStep * 2 + 16;
+template <int HS> constexpr int k_bytes() { return kStep * k_stride<HS>(); }
+template <int HS> constexpr int v_bytes() { return HS * kVStride; }
+// Beside K and V, for each of the two buffers: which of a step's 16-token blocks have a page (a byte each), whether a wave brought
+// NaN values (a byte each), and where they are (16 bits for each column and block).
+struct Marks { uint8_t there[4], unused[4], nan[kThreads / 64]; };
+template <int HS> struct Lds {
+  alignas(16) char k[2][k_bytes<HS>()];
+  alignas(16) char v[2][v_bytes<HS>()];
+  alignas(16) Marks marks[2];
+  alignas(8) uint16_t nan[2][HS][4];
+  Shares<kThreads> shares;
+};
+
+template <int HS>
+struct RowsWalk {
+  static constexpr int KS = HS / 16, EB = HS / 32;
+  // A wave brings 16-byte pieces of one 16-token block of a step, which lies in one piece of memory: hs 128 of K and V, hs 64 of
+  // one of the two.
+  static constexpr bool kBoth = HS == 128;
+  static constexpr int kPieces = HS;          // of a block
+  const CacheAttnArgs& a;
+  Lds<HS>& lds;
+  const int tid, wave, c, h;                  // c: the lane's row of the wave's 32, h: which half of the wave
+  const int block, piece;
+
+  __device__ RowsWalk(const CacheAttnArgs& args, Lds<HS>& shared)
+      : a(args), lds(shared), tid(threadIdx.x), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), c(threadIdx.x & 31), h((threadIdx.x >> 5) & 1),
+        block(kBoth ? wave >> 1 : wave & 3), piece(threadIdx.x % kPieces) {}
+
+  __device__ bool brings_k() const { return kBoth || wave < 4; }
+  __device__ bool brings_v() const { return kBoth || wave >= 4; }
+
+  // (A page that is not there reads page 0, unconditionally: a load under a condition would be waited for where it stands.)
+  struct Piece { u32x4 codes; uint32_t scale; };
+  __device__ Piece load(const uint8_t* codes, const uint8_t* scales, int number, int step, int head) const {
+    const int64_t place = (int64_t)(number < 0 ? 0 : number) * a.hk + head;
+    const int inside = (step * kStep + block * 16) & ((1 << a.page_shift) - 1);
+    return Piece{*(const u32x4*)(codes + ((place << a.page_shift) + inside) * HS + piece * 16), scales[place]};
+  }
+  // The page of the wave's block of a step; blocks behind the last one that counts are taken for that one.
+  __device__ int find(const int32_t* row, int step, int vis) const {
+    return __builtin_amdgcn_readfirstlane(row[cache_entry(step * 4 + block, vis, a.page_shift)]);
+  }
+
+  __device__ void put_k(const Piece& x, int buffer) const {
+    const float scale = scale_of(x.scale);
+    const int key = block * 16 + piece / (HS / 16), at = piece % (HS / 16) * 32;
+    bf16x8* const to = (bf16x8*)(lds.k[buffer] + key * k_stride<HS>() + at);
+    to[0] = widened(x.codes[0], x.codes[1], scale);
+    to[1] = widened(x.codes[2], x.codes[3], scale);
+  }
+  // `left`: how many of the block's tokens count.  What stands behind them counts as zero, whatever it is; NaN, too, which is
+  // kept apart: 0 times it would be NaN for rows that do not see it.
+  __device__ void put_v(const Piece& x, int buffer, int left) const {
+    const float scale = left > 0 ? scale_of(x.scale) : 1.0f;      // (0 times the NaN of a page in no use would be NaN)
+    u32x4 y = x.codes;
+    if (left < 16) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) y[w] &= first_bytes(left - 4 * w);
+    }
+    const uint32_t any = nan_codes(y[0]) | nan_codes(y[1]) | nan_codes(y[2]) | nan_codes(y[3]);
+    const bool some = __ballot(any != 0) != 0;
+    uint32_t where = 0;
+    if (some) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t n = nan_codes(y[w]) >> 7;
+        where |= ((n | n >> 7 | n >> 14 | n >> 21) & 15) << (4 * w);
+        y[w] &= ~(n * 0xff);
+      }
+    }
+    bf16x8* const to = (bf16x8*)(lds.v[buffer] + piece * kVStride + block * 32);
+    to[0] = widened(y[0], y[2], scale);
+    to[1] = widened(y[1], y[3], scale);
+    lds.nan[buffer][piece][block] = (uint16_t)where;
+    if ((tid & 63) == 0) {
+      lds.marks[buffer].nan[wave] = some;
+      lds.marks[buffer].there[block] = left > 0;
+    }
+  }
+
+  __device__ bf16x8 k_operand(int buffer, int kb, int ks) const {
+    return *(const bf16x8*)(lds.k[buffer] + (kb * 32 + c) * k_stride<HS>() + ks * 32 + h * 16);
+  }
+  __device__ bf16x8 v_operand(int buffer, int eb, int j) const {
+    return *(const bf16x8*)(lds.v[buffer] + (eb * 32 + c) * kVStride + j * 32 + h * 16);
+  }
+
+  // state of a unit's walk
+  bf16x8 q[KS];
+  f32x16 o[EB];
+  float m, l;
+  int limit, vis_wave, vis_first;      // keys that the lane's row sees; that the wave's last and first rows see
+
+  __device__ __forceinline__ void scores(int buffer, f32x16 (&x)[2]) const {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16 y = {};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(buffer, kb, ks), q[ks], y, 0, 0, 0);
+      x[kb] = y;
+    }
+  }
+
+  // The vector work and products of step s, whose scores are x, and the scores of step s + 1 into y (behind the last step: of
+  // what the buffer holds, for nobody).
+  __device__ __forceinline__ void compute(int s, f32x16 (&x)[2], f32x16 (&y)[2]) {
+    const u32x4 marks = *(const u32x4*)&lds.marks[s & 1];
+    const uint32_t mask = __builtin_amdgcn_readfirstlane(marks[0]), nan = __builtin_amdgcn_readfirstlane(marks[2] | marks[3]);
+    const bool cut = (s + 1) * kStep > vis_first;
+    if (cut || mask != 0x01010101) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int in = kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
+          if (s * kStep + in >= limit || !(mask >> (in / 16 * 8) & 1)) x[kb][i] = -INFINITY;
+        }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+    top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2e;
+    // The value that is subtracted need not be the maximum: it moves where a row's grows by more than 2^8.
+    if (__ballot(top > m + 8.0f)) {
+      const float now = fmaxf(m, top), use = now == -INFINITY ? 0.0f : now, alpha = exp2f(m - use);
+      m = now;
+      l *= alpha;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) o[eb] *= alpha;
+    }
+    const float use = m == -INFINITY ? 0.0f : m;
+    scores((s + 1) & 1, y);
+    bf16x8 p[4];
+    float sum = 0.0f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float w = __builtin_amdgcn_exp2f(x[kb][i] * a.scale_log2e - use);
+        sum += w;
+        p[kb * 2 + i / 8][i % 8] = (__bf16)w;
+      }
+    l += sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(s & 1, eb, j), p[j], o[eb], 0, 0, 0);
+    if (nan) {      // rows that see a NaN value are NaN in its column
+      uint64_t seen = 0;
+      for (int b = 0; b < 4; ++b) {
+        const int n = limit - s * kStep - 16 * b;
+        if (mask >> (8 * b) & 1) seen |= (uint64_t)(n >= 16 ? 0xffff : n <= 0 ? 0 : (1 << n) - 1) << (16 * b);
+      }
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (*(const uint64_t*)lds.nan[s & 1][eb * 32 + 8 * (i / 4) + 4 * h + i % 4] & seen) o[eb][i] = NAN;
+    }
+  }
+
+  // Steps [s0, s1) of a unit: results to o and lse if these are all, else to the partial result `slot`.
+  __device__ __forceinline__ void unit(const CacheUnits& u, int seq, int head, int tile, int s0, int s1, bool whole, float* slot) {
+    const int32_t* const row = a.block_table + (int64_t)seq * a.max_pages;
+    const int rows = u.rows(a, tile, kCacheRowsTile);
+    const int64_t row_first = (int64_t)tile * kCacheRowsTile;
+    const int vis = u.seen_by((row_first + rows - 1) / a.group);
+    const int end = (vis + kStep - 1) / kStep < s1 ? (vis + kStep - 1) / kStep : s1;
+    const int mine = wave * kRows + c, wave_rows = rows - wave * kRows < kRows ? rows - wave * kRows : kRows;
+    const int64_t row_wave = row_first + wave * kRows;
+    const int token = (int)((row_first + mine) / a.group), hq = head * a.group + (int)(row_first + mine - (int64_t)token * a.group);
+    vis_wave = wave_rows > 0 ? __builtin_amdgcn_readfirstlane(u.seen_by((row_wave + wave_rows - 1) / a.group)) : 0;
+    vis_first = wave_rows > 0 ? __builtin_amdgcn_readfirstlane(u.seen_by(row_wave / a.group)) : 0;
+    limit = mine < rows ? u.seen_by(token) : vis_wave;
+    m = -INFINITY;
+    l = 0.0f;
+    const __bf16* const from = (const __bf16*)a.q + (int64_t)(u.cu + token) * a.q_stride + hq * HS + h * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[ks] = mine < rows ? *(const bf16x8*)(from + ks * 16) : bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int eb = 0; eb < EB; ++eb) o[eb] = f32x16{};
+    if (s0 < end) {
+      const auto at_most = [&](int s) { return s < end ? s : end - 1; };
+      const auto counts = [&](int number, int step) { return cache_counts(step * 4 + block, vis, number, a.pages) ? vis - step * kStep - block * 16 : 0; };
+      const auto page_of = [&](int number) { return number >= 0 && number < a.pages ? number : 0; };
+      // numbers of the pages of the wave's block in this step and the next three
+      int n0 = find(row, s0, vis), n1 = find(row, at_most(s0 + 1), vis), n2 = find(row, at_most(s0 + 2), vis);
+      {
+        Piece k0 = {}, k1 = {}, v0 = {};
+        if (brings_k()) {
+          k0 = load(a.k_codes, a.k_scale, page_of(n0), s0, head);
+          k1 = load(a.k_codes, a.k_scale, page_of(n1), at_most(s0 + 1), head);
+        }
+        if (brings_v()) v0 = load(a.v_codes, a.v_scale, page_of(n0), s0, head);
+        __syncthreads();                            // the unit before has been read
+        if (brings_k()) {
+          put_k(k0, s0 & 1);
+          put_k(k1, (s0 + 1) & 1);
+        }
+        if (brings_v()) put_v(v0, s0 & 1, counts(n0, s0));
+      }
+      __syncthreads();
+      f32x16 x[2], y[2];
+      scores(s0 & 1, x);
+      __syncthreads();                              // (the first step's scores have been formed: its K makes room below)
+      int s = s0;
+      const auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2]) __attribute__((always_inline)) {
+        const int sk = at_most(s + 2), sv = at_most(s + 1);
+        Piece kk = {}, vv = {};
+        if (brings_k()) kk = load(a.k_codes, a.k_scale, page_of(n2), sk, head);
+        if (brings_v()) vv = load(a.v_codes, a.v_scale, page_of(n1), sv, head);
+        const int left = counts(n1, sv);
+        n1 = n2;
+        n2 = find(row, at_most(s + 3), vis);
+        if (s * kStep < vis_wave) compute(s, now, next);
+        if (brings_k()) put_k(kk, s & 1);
+        if (brings_v()) put_v(vv, (s + 1) & 1, left);
+        __syncthreads();
+        return ++s < end;
+      };
+      while (step(x, y) && step(y, x)) {
+      }
+    }
+    l += __shfl_xor(l, 32);
+    if (mine >= rows) return;
+    if (whole) {
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      const int64_t to = ((int64_t)(u.cu + token) * (a.hk * a.group) + hq) * HS + h * 4;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 w = f32x4{o[eb][4 * i], o[eb][4 * i + 1], o[eb][4 * i + 2], o[eb][4 * i + 3]} * inv;
+          if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to + eb * 32 + i * 8) = __builtin_convertvector(w, bf16x4);
+          else *(f32x4*)((float*)a.o + to + eb * 32 + i * 8) = w;
+        }
+      if (h == 0) a.lse[(int64_t)hq * a.total_q + u.cu + token] = natural_lse(m, l);
+    } else {
+      float* const to = slot + (int64_t)mine * (HS + 2);
+      if (h == 0) *(f32x2*)to = f32x2{m, l};
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *(f32x2*)(to + 2 + eb * 32 + i / 2 * 8 + h * 4 + i % 2 * 2) = f32x2{o[eb][2 * i], o[eb][2 * i + 1]};
+    }
+  }
+};
+
+template <int HS>
+__global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(CachePlan p) {
+  extern __shared__ __attribute__((aligned(16))) char dynamic[];
+  Lds<HS>& shared = *(Lds<HS>*)dynamic;
+  const Shares<kThreads>& shares = shared.shares;
+  const int64_t all = shared.shares.count(p.a, kCacheRowsTile);
+  // The workgroups of an XCD (blockIdx % 8) have shares that follow on one another: mostly of one KV head.
+  const int n = (int)gridDim.x, share = n % 8 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (n / 8) + (int)blockIdx.x / 8;
+  const int workers = all < n ? (int)all : n;
+  CacheLeft left = {0, -1, 0, 0};
+  if (share < workers) {
+    RowsWalk<HS> walk(p.a, shared);
+    float* const slots = p.partial + (int64_t)share * 2 * kCacheRowsTile * (HS + 2);
+    shares.walk(p.a, kCacheRowsTile, all * share / workers, all * (share + 1) / workers,
+                [&](const CacheUnits& u, int seq, const CacheUnits::Place& at, int end, int of) __attribute__((always_inline)) {
+                  const bool begins = at.step == 0, ends = end == of;
+                  walk.unit(u, seq, at.head, at.tile, at.step, end, begins && ends, slots + (begins ? kCacheRowsTile * (HS + 2) : 0));
+                  if (!begins) left.first = ends ? 2 : 1;
+                  else if (!ends) left.seq = seq, left.head = at.head, left.tile = at.tile;
+                });
+  }
+  if (threadIdx.x == 0) p.left[share] = left;
+}
+
+template <int HS>
+int launch(const CachePlan& p, hipStream_t stream) {
+  static LdsLimitRaised raised;
+  if (!raise_dynamic_lds_limit((const void*)cache_attn_rows_kernel<HS>, sizeof(Lds<HS>), raised)) return USP_ERR_LAUNCH;
+  cache_attn_rows_kernel<HS><<<dim3(p.workers), kThreads, sizeof(Lds<HS>), stream>>>(p);
+  return USP_OK;
+}
+
+}  // namespace
+
+int launch_cache_attn_rows(const CachePlan& p, hipStream_t stream) { return p.a.hs == 128 ? launch<128>(p, stream) : launch<64>(p, stream); }
+
+}  // namespace usp

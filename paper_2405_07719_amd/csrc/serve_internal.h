@@ -30,8 +30,9 @@ struct CacheExtendArgs {
 int launch_cache_extend(const CacheExtendArgs& a, hipStream_t stream);
 
 // Exponents of a page's scale: with the smallest, 2^-9 (the least code) times it is still a normal bf16 and fp32 number; with
-// the largest, the sum of 2^23 values of 448 times it is still finite (attention divides by the sum of its weights at the end).
-constexpr int kCacheMinExp = -117, kCacheMaxExp = 96;
+// the largest, the sum of 2^23 values of 448 times it, with weights of up to 2^8, is still finite (attention divides by the sum of its
+// weights at the end).
+constexpr int kCacheMinExp = -117, kCacheMaxExp = 88;
 
 struct CacheAppendArgs {
   const void* x[2];            // K, V
@@ -112,13 +113,30 @@ struct CacheUnits {
   }
 };
 
-// Page of 16-key block b of a request whose row of the table is `row`, -1 where none of its keys counts: behind the first `vis`
-// keys, or on another rank, or no page of the cache.
-__host__ __device__ inline int cache_page(const CacheAttnArgs& a, const int32_t* row, int b, int vis) {
-  if ((int64_t)b * 16 >= vis) return -1;
-  const int number = row[b >> (a.page_shift - 4)];
-  return number >= 0 && number < a.pages ? number : -1;
+// Where the page number of 16-key block b stands in a request's row of the table, of which the first `vis` keys count, vis >= 1;
+// blocks behind the last that counts are looked up as that one, so that the lookup needs no condition.
+__host__ __device__ inline int cache_entry(int b, int vis, int page_shift) {
+  const int last = (vis - 1) / 16;
+  return (b < last ? b : last) >> (page_shift - 4);
 }
+// Whether block b counts and `number` is a page of the cache.
+__host__ __device__ inline bool cache_counts(int b, int vis, int number, int64_t pages) {
+  return (int64_t)b * 16 < vis && number >= 0 && number < pages;
+}
+
+// What a worker (a wave, or a workgroup) leaves for the joining launch: `first`: 0, or its share begins inside a unit, which goes
+// on behind it (1) or ends in it (2); seq >= 0: its share ends inside the unit (seq, head, tile), which begins in it.
+struct CacheLeft { int first, seq, head, tile; };
+
+struct CachePlan {
+  CacheAttnArgs a;
+  int workers;         // shares, at most
+  CacheLeft* left;     // [workers]
+  float* partial;      // [workers][2][rows of a tile][hs + 2]: per row m, l, then O; [0]: the unit that began before the share
+};
+
+constexpr int kCacheRowsTile = 256;      // rows of a unit of the kernel for many rows
+int launch_cache_attn_rows(const CachePlan& p, hipStream_t stream);
 int launch_cache_attn(const CacheAttnArgs& a, int max_q, hipStream_t stream);
 size_t cache_attn_workspace(int group, int hs, int max_q);
 

@@ -89,7 +89,7 @@ def same_codes(a, b):
 
 
 def exponent(most):
-    """Smallest e with most <= 448 * 2^e, within [-117, 96]."""
+    """Smallest e with most <= 448 * 2^e, within [-117, 88]."""
     if most == 0:
         return -117
     e = int(np.ceil(np.log2(most / 448.0)))
@@ -97,7 +97,7 @@ def exponent(most):
         e -= 1
     while most > 448.0 * 2.0 ** e:
         e += 1
-    return max(-117, min(96, e))
+    return max(-117, min(88, e))
 
 
 def v_rows(v):

@@ -130,7 +130,7 @@ def test_cache_refusals(lib):
 def test_attention_workspace_depends_on_the_rows_of_a_tile_alone(lib):
     sizes = {(hs, hq, mq): usp.usp_cache_attn_workspace_bytes(cache(hs=hs), hq, mq) for hs in (64, 128) for hq in (2, 8, 64) for mq in (0, 1, 4, 5, 9, 4096)}
     assert max(sizes.values()) <= 96 << 20
-    assert sizes[128, 8, 1] == sizes[128, 8, 0] == sizes[128, 8, 4] == usp.usp_cache_attn_workspace_bytes(cache(pages=1000, page=128, hk=4), 16, 2)
+    assert sizes[128, 8, 1] == sizes[128, 8, 0] == sizes[128, 8, 4] == usp.usp_cache_attn_workspace_bytes(cache(pages=1000, page=128, hk=4), 16, 4)
 
 
 PLAN = """
@@ -186,10 +186,10 @@ extern "C" int walk(const int32_t* cu, const int32_t* lens, int n, int64_t total
   return open ? 8 : 0;
 }
 extern "C" int page_at(const int32_t* row, int b, int vis, int shift, int64_t pages) {
-  CacheAttnArgs a = {};
-  a.page_shift = shift; a.pages = pages;
-  return cache_page(a, row, b, vis);
+  const int number = row[cache_entry(b, vis, shift)];
+  return cache_counts(b, vis, number, pages) ? number : -1;
 }
+extern "C" int entry_at(int b, int vis, int shift) { return cache_entry(b, vis, shift); }
 """
 
 
@@ -209,7 +209,7 @@ def walked(plan, cu, lens, group, hk, max_pages, shift, causal, rt, waves, total
 
 
 @pytest.mark.parametrize("causal", [0, 1])
-@pytest.mark.parametrize("rt,waves", [(16, 2048), (32, 2048), (64, 1024), (16, 3)])
+@pytest.mark.parametrize("rt,waves", [(16, 2048), (256, 256), (16, 3)])
 def test_every_key_is_walked_once(plan, causal, rt, waves):
     rng = np.random.default_rng(rt + waves + causal)
     for _ in range(60):
@@ -239,7 +239,7 @@ def test_lengths_that_lie_are_held_within_the_table(plan):
     assert keys.tolist() == [3 * 50, 0, 4 * 50]
     assert walked(plan, [0, 0], [0], 1, 1, 1, 4, 1, 16, 2048)[0].tolist() == [0]
     # the longest that there can be: counts pass 32 bits
-    keys, _ = walked(plan, [0, 70000], [big], 1, 8, 2 ** 24, 7, 0, 64, 1024)
+    keys, _ = walked(plan, [0, 70000], [big], 1, 8, 2 ** 24, 7, 0, 256, 256)
     assert keys[0] == big * 70000 * 8
 
 
@@ -249,4 +249,6 @@ def test_pages_that_are_none(plan):
     pages = lambda b, vis=10 ** 6, shift=5: plan.page_at(ptr, b, vis, shift, ctypes.c_int64(10))  # noqa: E731
     assert [pages(b) for b in range(12)] == [3, 3, -1, -1, 9, 9, -1, -1, -1, -1, -1, -1]
     assert [pages(b, 17) for b in range(4)] == [3, 3, -1, -1]
-    assert plan.page_at(None, 5, 80, 4, ctypes.c_int64(10)) == -1     # behind the last key the table is not read
+    for shift in range(4, 8):          # no entry behind the last page with a key that counts is read
+        for vis in (1, 15, 16, 17, 127, 128, 129, 2 ** 31 - 1):
+            assert all(0 <= plan.entry_at(b, vis, shift) <= (vis - 1) >> shift for b in (0, 1, 7, 8, 9, 2 ** 27 - 1))
