@@ -1,24 +1,25 @@
 // Attention over the 8-bit cache: rows of ragged requests against their cached tokens.
 //
-// A unit is one request, KV head and tile of RT = 16 R rows (tokens x query heads of the KV head, so the query heads that
-// share K and V share one read of them); its keys are walked in steps of 64.  All steps of all units, laid one behind the
-// other, are cut evenly among the waves of the launch, whatever the lengths: every wave works out from the lengths, which
-// stand on the device, where its share begins.  A unit that lies within one wave's share is finished there; one that is cut
-// leaves partial results (maximum, sum, unnormalised output), of which a wave has two at most - the end of a unit that
-// began before its share, and the beginning of one that goes on behind it - and a second launch joins them, in the order
-// of the keys.
+// A unit is one request, KV head and tile of 16 rows (tokens x query heads of the KV head, so the query heads that share K and
+// V share one read of them); its keys are walked in steps of 64.  All steps of all units, laid one behind the other, are cut
+// evenly among one workgroup per CU, and a workgroup's share among its eight waves, whatever the lengths: every workgroup works
+// out from the lengths, which stand on the device, where its share begins.  A unit that lies within one wave's share is finished
+// there.  Of one that is cut, the wave that has its beginning keeps its result (maximum, sum, unnormalised output) in
+// registers, the waves behind it put theirs into LDS, and the first adds them up in the order of the keys.  Units cut between
+// workgroups leave partial results to a joining launch, two to a workgroup at most: the end of a unit that began before its share,
+// and the beginning of one that goes on behind it.
 //
 // The products are those of S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row's scores and its output elements
 // all along: row c = lane % 16, keys and elements by g = lane / 16.  Row 4 g' + r of the t-th 16-key product of a step
 // is key 16 g' + 4 t + r, which gives lane group g the 16 keys of one block of the cache: its P is, as it stands, the
-// operand of the second product, whose V operand is 16 bytes of one column of a V tile.  Nothing goes through LDS.
+// operand of the second product, whose V operand is 16 bytes of one column of a V tile.  Codes go from memory to registers to
+// the matrix cores, not through LDS.
 #include "cache_attn_device.h"
 
 namespace usp {
 namespace {
 
-constexpr int kThreads = 256, kStep = kCacheStep;
-typedef CacheUnits Units;
+constexpr int kThreads = 512, kWaves = kThreads / 64, kStep = kCacheStep, kTile = 16, kJoinThreads = 256;
 
 __device__ inline float group_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -29,9 +30,11 @@ __device__ inline float group_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-template <int HS, int R>
+template <int HS>
 struct Walk {
-  static constexpr int RT = 16 * R, KI = HS / 32, ET = HS / 16, KV16 = HS / 64;     // KV16: 16-byte reads of a K row's quarter
+  static constexpr int KI = HS / 32, ET = HS / 16, KV16 = HS / 64;     // KV16: 16-byte reads of a K row's quarter
+  // A partial result in LDS: m and l of each row, then O, rows 16 bytes further apart than in memory (banks).
+  static constexpr int kLdsRow = HS + 4, kLdsSlot = kTile * (kLdsRow + 2);
   const CachePlan& p;
   int lane, c, g;
 
@@ -69,31 +72,30 @@ struct Walk {
     vs = p.a.v_scale[place];
   }
 
-  // Steps [s0, s1) of a unit of `steps` ones: results to o and lse if these are all, else to partial result `slot`.
-  __device__ void unit(const Units& u, int seq, int head, int tile, int s0, int s1, bool whole, float* slot) {
+  // the unit that is walked, or was last
+  bf16x8 q[KI];
+  f32x4 o[ET];
+  float m, l;                  // l: the lane's part of the row's sum
+  int rows, token, hq;         // rows of the tile; the lane's row: its token (of all) and query head
+
+  // Steps [s0, s1) of a unit.
+  __device__ __forceinline__ void unit(const CacheUnits& u, int seq, int head, int tile, int s0, int s1) {
     const CacheAttnArgs& a = p.a;
     const int32_t* const row = a.block_table + (int64_t)seq * a.max_pages;
-    const int rows = u.rows(a, tile, RT);
+    rows = u.rows(a, tile, kTile);
     // keys that the tile's first and last rows see
-    const int64_t row_first = (int64_t)tile * RT;
+    const int64_t row_first = (int64_t)tile * kTile;
     const int vis = u.seen_by((row_first + rows - 1) / a.group), vis_first = u.seen_by(row_first / a.group);
-    int limit[R];
-    bf16x8 q[R][KI];
-    f32x4 o[R][ET];
-    float m[R], l[R];
+    const int in = (int)((row_first + c) / a.group), limit = c < rows ? u.seen_by(in) : vis;
+    token = u.cu + in;
+    hq = head * a.group + (int)(row_first + c - (int64_t)in * a.group);
+    m = -INFINITY;
+    l = 0.0f;
+    const __bf16* const from = (const __bf16*)a.q + (int64_t)token * a.q_stride + hq * HS + g * (HS / 4);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int at = r * 16 + c, token = (int)((row_first + at) / a.group), h = (int)(row_first + at - (int64_t)token * a.group);
-      limit[r] = at < rows ? u.seen_by(token) : vis;
-      m[r] = -INFINITY;
-      l[r] = 0.0f;
-      const __bf16* const from = (const __bf16*)a.q + (int64_t)(u.cu + token) * a.q_stride + (head * a.group + h) * HS + g * (HS / 4);
+    for (int i = 0; i < KI; ++i) q[i] = c < rows ? *(const bf16x8*)(from + i * 8) : bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < KI; ++i)
-        q[r][i] = at < rows ? *(const bf16x8*)(from + i * 8) : bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-      for (int e = 0; e < ET; ++e) o[r][e] = f32x4{0, 0, 0, 0};
-    }
+    for (int e = 0; e < ET; ++e) o[e] = f32x4{0, 0, 0, 0};
     const int end = (vis + kStep - 1) / kStep < s1 ? (vis + kStep - 1) / kStep : s1;
     if (s0 < end) {
       find(row, s0, vis);
@@ -106,59 +108,46 @@ struct Walk {
       if (more) find(row, s + 1, vis);
       const float scale_k = scale_of(ks);
       // S^T = K Q^T
-      f32x4 x[R][4];
+      f32x4 x[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
+        x[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int r = 0; r < R; ++r) x[r][t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < KI; ++i) {
-          const bf16x8 w = widened(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1], scale_k);
-#pragma unroll
-          for (int r = 0; r < R; ++r) x[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, q[r][i], x[r][t], 0, 0, 0);
-        }
+        for (int i = 0; i < KI; ++i)
+          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1], scale_k), q[i], x[t], 0, 0, 0);
       }
       if (more) load_k(s + 1, head);
       const int key0 = s * kStep + g * 16;            // the lane's first key
-      const bool missing = __ballot(!valid) != 0, masked = (s + 1) * kStep > vis_first || missing;
-      if (masked) {
+      const bool missing = __ballot(!valid) != 0, cut = (s + 1) * kStep > vis_first;
+      if (cut || missing) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!valid || key0 + 4 * t + e >= limit[r]) x[r][t][e] = -INFINITY;
+          for (int e = 0; e < 4; ++e)
+            if (!valid || key0 + 4 * t + e >= limit) x[t][e] = -INFINITY;
       }
-      bf16x8 pr[R][2];
+      float top = x[0][0];
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float top = x[r][0][0];
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, x[t][e]);
+      top = group_max(top) * a.scale_log2e;
+      const float now = fmaxf(m, top), use = now == -INFINITY ? 0.0f : now, alpha = exp2f(m - use);
+      m = now;
+      float sum = 0.0f;
+      bf16x8 pr[2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top = fmaxf(top, x[r][t][e]);
-        top = group_max(top) * a.scale_log2e;
-        const float now = fmaxf(m[r], top), use = now == -INFINITY ? 0.0f : now;
-        const float alpha = exp2f(m[r] - use);
-        m[r] = now;
-        float sum = 0.0f;
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[r][t][e] = __builtin_amdgcn_exp2f(x[r][t][e] * a.scale_log2e - use);
-            sum += x[r][t][e];
-          }
-        l[r] = l[r] * alpha + sum;
-        if (__ballot(alpha != 1.0f)) {
-#pragma unroll
-          for (int e = 0; e < ET; ++e) o[r][e] *= alpha;
+        for (int e = 0; e < 4; ++e) {
+          const float w = __builtin_amdgcn_exp2f(x[t][e] * a.scale_log2e - use);
+          sum += w;
+          pr[t / 2][t % 2 * 4 + e] = (__bf16)w;       // (bf16 is what the matrix cores take: half a step is 2^-8 of a weight)
         }
+      l = l * alpha + sum;
+      if (__ballot(alpha != 1.0f)) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pr[r][j][e] = (__bf16)x[r][2 * j + e / 4][e % 4];
+        for (int e = 0; e < ET; ++e) o[e] *= alpha;
       }
       // what stands behind the last key, or in a page that is not there, counts as zero, whatever it is
       if ((s + 1) * kStep > vis || missing) {
@@ -172,13 +161,18 @@ struct Walk {
       }
       // NaN in a value that some rows of the tile see and others do not: 0 times it would be NaN for those.  Counted apart,
       // with another product, and taken as zero in the one that counts.
-      if (vis_first < vis && (s + 1) * kStep > vis_first) {
+      if (cut && vis_first < vis) {
         uint32_t any = 0;
 #pragma unroll
         for (int e = 0; e < ET; ++e)
 #pragma unroll
           for (int w = 0; w < 4; ++w) any |= nan_codes(v[e][w]);
         if (__ballot(any != 0)) {
+          bf16x8 sees[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int b = 0; b < 8; ++b) sees[j][b] = (__bf16)(valid && key0 + 8 * j + b < limit ? 1.0f : 0.0f);
 #pragma unroll
           for (int e = 0; e < ET; ++e) {
             bf16x8 is[2];
@@ -189,20 +183,12 @@ struct Walk {
               for (int b = 0; b < 4; ++b) is[w / 2][w % 2 * 4 + b] = (__bf16)((n >> (8 * b + 7)) & 1 ? 1.0f : 0.0f);
               v[e][w] &= ~((n >> 7) * 0xffu);
             }
+            f32x4 count = {0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-              f32x4 count = {0, 0, 0, 0};
+            for (int j = 0; j < 2; ++j) count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is[j], sees[j], count, 0, 0, 0);
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                bf16x8 sees;
-#pragma unroll
-                for (int b = 0; b < 8; ++b) sees[b] = (__bf16)(valid && key0 + 8 * j + b < limit[r] ? 1.0f : 0.0f);
-                count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is[j], sees, count, 0, 0, 0);
-              }
-#pragma unroll
-              for (int b = 0; b < 4; ++b)
-                if (count[b] > 0.0f) o[r][e][b] = NAN;
-            }
+            for (int b = 0; b < 4; ++b)
+              if (count[b] > 0.0f) o[e][b] = NAN;
           }
         }
       }
@@ -211,127 +197,217 @@ struct Walk {
 #pragma unroll
       for (int e = 0; e < ET; ++e)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const bf16x8 w = widened(v[e][2 * j], v[e][2 * j + 1], scale_v);
-#pragma unroll
-          for (int r = 0; r < R; ++r) o[r][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, pr[r][j], o[r][e], 0, 0, 0);
-        }
+        for (int j = 0; j < 2; ++j)
+          o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(v[e][2 * j], v[e][2 * j + 1], scale_v), pr[j], o[e], 0, 0, 0);
       if (more) load_v(s + 1, head);
     }
+    l = group_sum(l);
+  }
+
+  __device__ void write() const {
+    if (c >= rows) return;
+    const CacheAttnArgs& a = p.a;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t to = ((int64_t)token * (a.hk * a.group) + hq) * HS + g * 4;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      l[r] = group_sum(l[r]);
-      const int at = r * 16 + c;
-      if (at >= rows) continue;
-      if (whole) {
-        const int token = (int)((row_first + at) / a.group), h = head * a.group + (int)(row_first + at - (int64_t)token * a.group);
-        const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
-        const int64_t to = ((int64_t)(u.cu + token) * (a.hk * a.group) + h) * HS + g * 4;
-#pragma unroll
-        for (int e = 0; e < ET; ++e) {
-          const f32x4 y = o[r][e] * inv;
-          if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to + e * 16) = __builtin_convertvector(y, bf16x4);
-          else *(f32x4*)((float*)a.o + to + e * 16) = y;
-        }
-        if (g == 0) a.lse[(int64_t)h * a.total_q + u.cu + token] = natural_lse(m[r], l[r]);
-      } else {
-        float* const to = slot + (int64_t)at * (HS + 2);
-        if (g == 0) *(f32x2*)to = f32x2{m[r], l[r]};
-#pragma unroll
-        for (int e = 0; e < ET; ++e) {
-          *(f32x2*)(to + 2 + e * 16 + g * 4) = f32x2{o[r][e][0], o[r][e][1]};
-          *(f32x2*)(to + 4 + e * 16 + g * 4) = f32x2{o[r][e][2], o[r][e][3]};
-        }
-      }
+    for (int e = 0; e < ET; ++e) {
+      const f32x4 y = o[e] * inv;
+      if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to + e * 16) = __builtin_convertvector(y, bf16x4);
+      else *(f32x4*)((float*)a.o + to + e * 16) = y;
     }
+    if (g == 0) a.lse[(int64_t)hq * a.total_q + token] = natural_lse(m, l);
+  }
+  __device__ void put(float* slot, int row) const {
+    if (c >= rows) return;
+    if (g == 0) ((f32x2*)slot)[c] = f32x2{m, l};
+#pragma unroll
+    for (int e = 0; e < ET; ++e) *(f32x4*)(slot + 2 * kTile + c * row + e * 16 + g * 4) = o[e];
+  }
+  // what the next wave has of the same unit
+  __device__ void add(const float* slot) {
+    if (c >= rows) return;
+    const f32x2 other = ((const f32x2*)slot)[c];
+    const float top = fmaxf(m, other[0]), use = top == -INFINITY ? 0.0f : top;
+    const float keep = exp2f(m - use), take = exp2f(other[0] - use);
+    l = l * keep + other[1] * take;
+    m = top;
+#pragma unroll
+    for (int e = 0; e < ET; ++e) o[e] = o[e] * keep + *(const f32x4*)(slot + 2 * kTile + c * kLdsRow + e * 16 + g * 4) * take;
   }
 };
 
-template <int HS, int R>
+template <int HS> struct Lds {
+  alignas(16) float slot[kWaves][Walk<HS>::kLdsSlot];
+  int first[kWaves];              // as in CacheLeft, of a wave's share
+  Shares<kThreads> shares;
+};
+
+template <int HS>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
-  __shared__ Shares<kThreads> shares;
-  constexpr int RT = 16 * R;
-  const int64_t all = shares.count(p.a, RT);
-  const int wave = __builtin_amdgcn_readfirstlane(((int)threadIdx.x >> 6) * (int)gridDim.x + (int)blockIdx.x);
+  extern __shared__ __attribute__((aligned(16))) char dynamic[];
+  Lds<HS>& lds = *(Lds<HS>*)dynamic;
+  const Shares<kThreads>& shares = lds.shares;
+  const int64_t all = lds.shares.count(p.a, kTile);
+  const int share = (int)blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int workers = all < p.workers ? (int)all : p.workers;
-  CacheLeft left = {0, -1, 0, 0};
-  if (wave < workers) {
-    Walk<HS, R> walk(p, threadIdx.x & 63);
-    float* const slots = p.partial + (int64_t)wave * 2 * RT * (HS + 2);
-    shares.walk(p.a, RT, all * wave / workers, all * (wave + 1) / workers,
-                [&](const CacheUnits& u, int seq, const CacheUnits::Place& at, int end, int of) __attribute__((always_inline)) {
-                  const bool begins = at.step == 0, ends = end == of;
-                  walk.unit(u, seq, at.head, at.tile, at.step, end, begins && ends, slots + (begins ? RT * (HS + 2) : 0));
-                  if (!begins) left.first = ends ? 2 : 1;
-                  else if (!ends) left.seq = seq, left.head = at.head, left.tile = at.tile;
-                });
+  int64_t pos = share < workers ? all * share / workers : all, stop = share < workers ? all * (share + 1) / workers : all;
+  if (p.whole) {
+    pos = shares.unit_start(p.a, kTile, pos, all);
+    stop = shares.unit_start(p.a, kTile, stop, all);
   }
-  if ((threadIdx.x & 63) == 0 && wave < p.workers) p.left[wave] = left;
+  // (rounded up: the first wave has a step wherever the workgroup has one)
+  const int64_t mine = pos + ((stop - pos) * wave + kWaves - 1) / kWaves, next = pos + ((stop - pos) * (wave + 1) + kWaves - 1) / kWaves;
+  Walk<HS> walk(p, threadIdx.x & 63);
+  float* const slots = p.partial + share * 2 * CachePlan::slot(kTile, HS);
+  int first = 0, end_seq = -1, end_head = 0, end_tile = 0;      // as in CacheLeft, of the wave's share
+  shares.walk(p.a, kTile, mine, next, [&](const CacheUnits& u, int seq, const CacheUnits::Place& at, int end, int of) __attribute__((always_inline)) {
+    const bool begins = at.step == 0, ends = end == of;
+    walk.unit(u, seq, at.head, at.tile, at.step, end);
+    if (begins && ends) {
+      walk.write();
+    } else if (begins) {
+      end_seq = seq;
+      end_head = at.head;
+      end_tile = at.tile;
+    } else {
+      first = ends ? 2 : 1;
+      if (wave) walk.put(lds.slot[wave], Walk<HS>::kLdsRow);
+      else if (ends) walk.put(slots, HS);
+    }
+  });
+  // A wave without steps lets the unit that goes on around it pass (it has no partial result: 3).
+  if ((threadIdx.x & 63) == 0) lds.first[wave] = mine < next ? first : 3;
+  __syncthreads();
+  // The wave that has the beginning of a unit, or the workgroup's first part of one that began before, adds up what follows.
+  CacheLeft left = {wave == 0 ? first : 0, -1, 0, 0};
+  if (end_seq >= 0 || (wave == 0 && first == 1)) {
+    bool ended = false;
+    for (int w = wave + 1; w < kWaves && !ended; ++w) {
+      const int f = lds.first[w];
+      if (f == 1 || f == 2) walk.add(lds.slot[w]);
+      ended = f == 2;
+    }
+    if (end_seq < 0) {
+      walk.put(slots, HS);
+      left.first = ended ? 2 : 1;
+    } else if (ended) {
+      walk.write();
+    } else {
+      walk.put(slots + CachePlan::slot(kTile, HS), HS);
+      left.seq = end_seq, left.head = end_head, left.tile = end_tile;
+    }
+  }
+  if (p.whole) return;
+  // (one wave writes both parts of what the workgroup leaves: the last beginning may be any wave's)
+  __shared__ CacheLeft ends;
+  if (threadIdx.x == 0) ends.seq = -1;
+  __syncthreads();
+  if (left.seq >= 0 && (threadIdx.x & 63) == 0) ends = left;
+  __syncthreads();
+  if (threadIdx.x == 0) p.left[share] = CacheLeft{left.first, ends.seq, ends.head, ends.tile};
 }
 
 // Joins the partial results of one unit: the beginning that worker w left, then what the workers behind it left up to the unit's
-// end.  blockIdx.y: which of the unit's rows.
+// end.  A team of HS / 4 threads adds up a row, four columns to a thread; the teams of a workgroup share the parts of one
+// row where there are many, else they have a row each.  blockIdx.y: which of the unit's rows.
 template <int HS>
-__global__ __launch_bounds__(kThreads) void cache_attn_join_kernel(CachePlan p, int rows_per_tile) {
-  const int64_t slot = (int64_t)rows_per_tile * (HS + 2);
+__global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan p, int rows_per_tile) {
+  constexpr int kTeam = HS / 4, kTeams = kJoinThreads / kTeam;
+  __shared__ f32x4 sums[kTeams][kTeam];
+  const int64_t slot = CachePlan::slot(rows_per_tile, HS);
   const CacheAttnArgs& a = p.a;
-  const int w = blockIdx.x;
+  const int w = blockIdx.x, lane = threadIdx.x & 63, team = threadIdx.x / kTeam, e = threadIdx.x % kTeam * 4;
   const CacheLeft mine = p.left[w];
   if (mine.seq < 0) return;
+  int parts = 1;                                     // parts 1 .. parts - 1 are those of workers w + 1 ...
+  for (;;) {
+    const int x = w + parts + lane;
+    const uint64_t on = __ballot(x < p.workers && p.left[x < p.workers ? x : w].first == 1);
+    if (on != ~0ull) {
+      parts += __builtin_ctzll(~on);
+      break;
+    }
+    parts += 64;
+  }
+  parts += w + parts < p.workers;                    // the one in which it ends
   const CacheUnits u(a, mine.seq, rows_per_tile);
   const int rows = u.rows(a, mine.tile, rows_per_tile);
-  int last = w + 1;
-  while (last < p.workers - 1 && p.left[last].first == 1) ++last;
-  for (int i = blockIdx.y * kThreads + threadIdx.x; i < rows * HS; i += kThreads * gridDim.y) {
-    const int row = i / HS, e = i - row * HS;
-    const float* at = p.partial + (2 * (int64_t)w + 1) * slot + row * (HS + 2);
-    float m = at[0], l = at[1], o = at[2 + e];
-    for (int x = w + 1; x <= last; ++x) {
-      at = p.partial + 2 * (int64_t)x * slot + row * (HS + 2);
-      const float mx = at[0], lx = at[1], ox = at[2 + e];
-      const float top = fmaxf(m, mx), use = top == -INFINITY ? 0.0f : top;
-      const float keep = exp2f(m - use), add = exp2f(mx - use);
-      l = l * keep + lx * add;
+  const bool shared = parts >= kTeams;               // many parts to a row
+  const auto slot_of = [&](int x) { return p.partial + (x ? 2 * (int64_t)(w + x) : 2 * (int64_t)w + 1) * slot; };
+  const int step = shared ? gridDim.y : gridDim.y * kTeams;
+  for (int row = shared ? blockIdx.y : blockIdx.y * kTeams + team; row < rows; row += step) {
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int x = shared ? team : 0; x < parts; x += shared ? kTeams : 1) {
+      const float* const at = slot_of(x);
+      const f32x2 ml = ((const f32x2*)at)[row];
+      const f32x4 ox = *(const f32x4*)(at + 2 * rows_per_tile + row * HS + e);
+      const float top = fmaxf(m, ml[0]), use = top == -INFINITY ? 0.0f : top;
+      const float keep = exp2f(m - use), add = exp2f(ml[0] - use);
+      l = l * keep + ml[1] * add;
       o = o * keep + ox * add;
       m = top;
     }
+    if (shared) {                                    // the teams' sums, in their order
+      __shared__ f32x2 mls[kTeams];
+      __syncthreads();
+      sums[team][threadIdx.x % kTeam] = o;
+      if (e == 0) mls[team] = f32x2{m, l};
+      __syncthreads();
+      if (team) continue;
+      for (int t = 1; t < kTeams; ++t) {
+        const f32x2 ml = mls[t];
+        const float top = fmaxf(m, ml[0]), use = top == -INFINITY ? 0.0f : top;
+        const float keep = exp2f(m - use), add = exp2f(ml[0] - use);
+        l = l * keep + ml[1] * add;
+        o = o * keep + sums[t][threadIdx.x] * add;
+        m = top;
+      }
+    }
     const int64_t row_in = (int64_t)mine.tile * rows_per_tile + row;
     const int token = (int)(row_in / a.group), h = mine.head * a.group + (int)(row_in - (int64_t)token * a.group);
-    const float y = l == 0.0f ? 0.0f : o / l;
+    const f32x4 y = o * (l == 0.0f ? 0.0f : 1.0f / l);
     const int64_t to = ((int64_t)(u.cu + token) * (a.hk * a.group) + h) * HS + e;
-    if (a.o_dtype == USP_BF16) ((__bf16*)a.o)[to] = (__bf16)y;
-    else ((float*)a.o)[to] = y;
+    if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to) = __builtin_convertvector(y, bf16x4);
+    else *(f32x4*)((float*)a.o + to) = y;
     if (e == 0) a.lse[(int64_t)h * a.total_q + u.cu + token] = natural_lse(m, l);
   }
 }
 
-// Up to 16 rows of a request fit one product of the kernel that has a wave to itself; more go to the kernel for many rows.
+// Up to 16 rows of a request fit one product of the kernel that gives each wave units of its own; more go to the kernel for many
+// rows.  Both have one workgroup of eight waves to a CU.
 bool few_rows(int group, int max_q) { return (int64_t)group * (max_q < 1 ? 1 : max_q) <= 16; }
-int rows_of(bool few) { return few ? 16 : kCacheRowsTile; }
-int workers_of(bool few) { return few ? kPlanCUs * 8 : kPlanCUs; }
+int rows_of(bool few) { return few ? kTile : kCacheRowsTile; }
+
+template <int HS>
+int launch_few(const CachePlan& p, hipStream_t stream) {
+  static LdsLimitRaised raised;
+  if (!raise_dynamic_lds_limit((const void*)cache_attn_kernel<HS>, sizeof(Lds<HS>), raised)) return USP_ERR_LAUNCH;
+  cache_attn_kernel<HS><<<dim3(p.workers), kThreads, sizeof(Lds<HS>), stream>>>(p);
+  return USP_OK;
+}
 
 }  // namespace
 
 size_t cache_attn_workspace(int group, int hs, int max_q) {
-  const bool few = few_rows(group, max_q);
-  return (size_t)workers_of(few) * (sizeof(CacheLeft) + (size_t)2 * rows_of(few) * (hs + 2) * sizeof(float));
+  return kPlanCUs * (sizeof(CacheLeft) + 2 * CachePlan::slot(rows_of(few_rows(group, max_q)), hs) * sizeof(float));
 }
 
 int launch_cache_attn(const CacheAttnArgs& a, int max_q, hipStream_t stream) {
   const bool few = few_rows(a.group, max_q);
-  CachePlan p = {a, workers_of(few), (CacheLeft*)a.workspace, nullptr};
+  CachePlan p = {a, kPlanCUs, (CacheLeft*)a.workspace, nullptr, 0};
   p.partial = (float*)(p.left + p.workers);
-  if (few) {
-    const dim3 grid(p.workers / (kThreads / 64));
-    if (a.hs == 128) cache_attn_kernel<128, 1><<<grid, kThreads, 0, stream>>>(p);
-    else cache_attn_kernel<64, 1><<<grid, kThreads, 0, stream>>>(p);
-  } else {
-    const int st = launch_cache_attn_rows(p, stream);
-    if (st != USP_OK) return st;
+  // Rows of the table that hold 4096 tokens at most: a wave has eight steps of a unit at most, and the joining launch would cost
+  // more than cutting units between workgroups gains.
+  p.whole = few && (int64_t)a.max_pages << a.page_shift <= 4096;
+  const int st = !few ? launch_cache_attn_rows(p, stream) : a.hs == 128 ? launch_few<128>(p, stream) : launch_few<64>(p, stream);
+  if (st != USP_OK) return st;
+  if (!p.whole) {
+    const dim3 grid(p.workers, few ? 4 : 16);
+    if (a.hs == 128) cache_attn_join_kernel<128><<<grid, kJoinThreads, 0, stream>>>(p, rows_of(few));
+    else cache_attn_join_kernel<64><<<grid, kJoinThreads, 0, stream>>>(p, rows_of(few));
   }
-  const dim3 grid(p.workers, few ? 1 : 8);
-  if (a.hs == 128) cache_attn_join_kernel<128><<<grid, kThreads, 0, stream>>>(p, rows_of(few));
-  else cache_attn_join_kernel<64><<<grid, kThreads, 0, stream>>>(p, rows_of(few));
   return launch_status();
 }
 

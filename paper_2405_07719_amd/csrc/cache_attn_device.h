@@ -38,12 +38,17 @@ template <int THREADS>
 struct Shares {
   int64_t before[THREADS + 1];     // steps of the requests before a thread's first one
   int64_t part[THREADS / 64];
+  CacheUnits::Request first[THREADS];   // each thread's first request
 
   // By all threads of a workgroup: the steps in all.  Each thread counts `n / THREADS` requests in a row.
   __device__ int64_t count(const CacheAttnArgs& a, int rows_per_tile) {
     const int tid = threadIdx.x, lane = tid & 63, n = a.n_seqs, per = (n + THREADS - 1) / THREADS;
     int64_t sum = 0;
-    for (int i = tid * per; i < (tid + 1) * per && i < n; ++i) sum += CacheUnits(a, i, rows_per_tile).per_head * a.hk;
+    for (int i = tid * per; i < (tid + 1) * per && i < n; ++i) {
+      const CacheUnits::Request r = CacheUnits::read(a, i);
+      if (i == tid * per) first[tid] = r;
+      sum += CacheUnits(a, r, rows_per_tile).per_head * a.hk;
+    }
     int64_t upto = sum, all = 0;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -63,29 +68,51 @@ struct Shares {
     return all;
   }
 
-  // The pieces of units that steps [pos, stop) are, one after the other: visit(units, seq, place, end step, whole unit's steps).
-  template <class Visit>
-  __device__ __forceinline__ void walk(const CacheAttnArgs& a, int rows_per_tile, int64_t pos, int64_t stop, Visit visit) const {
-    const int n = a.n_seqs, per = (n + THREADS - 1) / THREADS;
+  __device__ CacheUnits units(const CacheAttnArgs& a, int seq, int rows_per_tile) const {
+    return a.n_seqs <= THREADS ? CacheUnits(a, first[seq], rows_per_tile) : CacheUnits(a, seq, rows_per_tile);
+  }
+
+  struct Where { int seq; int64_t start; };      // a request, and its first step
+  __device__ __forceinline__ Where find(const CacheAttnArgs& a, int rows_per_tile, int64_t pos) const {
+    const int per = (a.n_seqs + THREADS - 1) / THREADS;
     int lo = 0, hi = THREADS;                    // the last thread whose first request begins at pos or before
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
       if (before[mid] <= pos) lo = mid;
       else hi = mid;
     }
-    int64_t start = before[lo];                  // where request `seq` begins
-    int seq = __builtin_amdgcn_readfirstlane(lo * per);
-    while (pos < stop && seq < n) {
-      const CacheUnits u(a, seq, rows_per_tile);
+    Where w = {__builtin_amdgcn_readfirstlane(lo * per), before[lo]};
+    for (; per > 1 && w.seq < a.n_seqs; ++w.seq) {
+      const int64_t steps = units(a, w.seq, rows_per_tile).per_head * a.hk;
+      if (pos < w.start + steps) break;
+      w.start += steps;
+    }
+    return w;
+  }
+
+  // The first step of the unit that step `pos` is of (the last step of all and one: itself).
+  __device__ __forceinline__ int64_t unit_start(const CacheAttnArgs& a, int rows_per_tile, int64_t pos, int64_t all) const {
+    if (pos >= all) return all;
+    const Where w = find(a, rows_per_tile, pos);
+    return pos - units(a, w.seq, rows_per_tile).locate(pos - w.start).step;
+  }
+
+  // The pieces of units that steps [pos, stop) are, one after the other: visit(units, seq, place, end step, whole unit's steps).
+  template <class Visit>
+  __device__ __forceinline__ void walk(const CacheAttnArgs& a, int rows_per_tile, int64_t pos, int64_t stop, Visit visit) const {
+    if (pos >= stop) return;
+    Where w = find(a, rows_per_tile, pos);
+    while (pos < stop && w.seq < a.n_seqs) {
+      const CacheUnits u = units(a, w.seq, rows_per_tile);
       const int64_t steps = u.per_head * a.hk;
-      if (pos >= start + steps) {
-        start += steps;
-        ++seq;
+      if (pos >= w.start + steps) {
+        w.start += steps;
+        ++w.seq;
         continue;
       }
-      const CacheUnits::Place at = u.locate(pos - start);
+      const CacheUnits::Place at = u.locate(pos - w.start);
       const int of = u.steps(at.tile), end = stop - pos < of - at.step ? at.step + (int)(stop - pos) : of;
-      visit(u, seq, at, end, of);
+      visit(u, w.seq, at, end, of);
       pos += end - at.step;
     }
   }

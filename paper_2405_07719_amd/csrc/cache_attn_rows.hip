@@ -263,12 +263,12 @@ struct RowsWalk {
         }
       if (h == 0) a.lse[(int64_t)hq * a.total_q + u.cu + token] = natural_lse(m, l);
     } else {
-      float* const to = slot + (int64_t)mine * (HS + 2);
-      if (h == 0) *(f32x2*)to = f32x2{m, l};
+      if (h == 0) ((f32x2*)slot)[mine] = f32x2{m, l};
+      float* const to = slot + 2 * kCacheRowsTile + mine * HS + h * 4;
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *(f32x2*)(to + 2 + eb * 32 + i / 2 * 8 + h * 4 + i % 2 * 2) = f32x2{o[eb][2 * i], o[eb][2 * i + 1]};
+        for (int i = 0; i < 4; ++i) *(f32x4*)(to + eb * 32 + i * 8) = f32x4{o[eb][4 * i], o[eb][4 * i + 1], o[eb][4 * i + 2], o[eb][4 * i + 3]};
     }
   }
 };
@@ -285,11 +285,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(CachePlan 
   CacheLeft left = {0, -1, 0, 0};
   if (share < workers) {
     RowsWalk<HS> walk(p.a, shared);
-    float* const slots = p.partial + (int64_t)share * 2 * kCacheRowsTile * (HS + 2);
+    float* const slots = p.partial + share * 2 * CachePlan::slot(kCacheRowsTile, HS);
     shares.walk(p.a, kCacheRowsTile, all * share / workers, all * (share + 1) / workers,
                 [&](const CacheUnits& u, int seq, const CacheUnits::Place& at, int end, int of) __attribute__((always_inline)) {
                   const bool begins = at.step == 0, ends = end == of;
-                  walk.unit(u, seq, at.head, at.tile, at.step, end, begins && ends, slots + (begins ? kCacheRowsTile * (HS + 2) : 0));
+                  walk.unit(u, seq, at.head, at.tile, at.step, end, begins && ends, slots + (begins ? CachePlan::slot(kCacheRowsTile, HS) : 0));
                   if (!begins) left.first = ends ? 2 : 1;
                   else if (!ends) left.seq = seq, left.head = at.head, left.tile = at.tile;
                 });

@@ -66,16 +66,17 @@ constexpr int kCacheStep = 64;
 struct CacheUnits {
   int cu, nq, len, tiles, base, each, causal;
   int64_t per_head;   // steps of one KV head's tiles
-  __host__ __device__ CacheUnits(const CacheAttnArgs& a, int i, int rows_per_tile) : causal(a.causal) {
+  struct Request { int cu, nq, len; };      // first row, rows, keys
+  __host__ __device__ static Request read(const CacheAttnArgs& a, int i) {
     const int total = (int)a.total_q;
     int c0 = a.cu_q[i], c1 = a.cu_q[i + 1];
     c0 = c0 < 0 ? 0 : c0 > total ? total : c0;
     c1 = c1 < c0 ? c0 : c1 > total ? total : c1;
-    cu = c0;
-    nq = c1 - c0;
     const int64_t room = (int64_t)a.max_pages << a.page_shift;
     const int x = a.kv_len[i];
-    len = x < 0 ? 0 : x > room ? (int)room : x;
+    return Request{c0, c1 - c0, x < 0 ? 0 : x > room ? (int)room : x};
+  }
+  __host__ __device__ CacheUnits(const CacheAttnArgs& a, const Request& r, int rows_per_tile) : cu(r.cu), nq(r.nq), len(r.len), causal(a.causal) {
     tiles = (int)(((int64_t)nq * a.group + rows_per_tile - 1) / rows_per_tile);
     each = 0;
     base = len ? (len - 1) / kCacheStep + 1 : 1;
@@ -85,6 +86,7 @@ struct CacheUnits {
     }
     per_head = upto(tiles);
   }
+  __host__ __device__ CacheUnits(const CacheAttnArgs& a, int i, int rows_per_tile) : CacheUnits(a, read(a, i), rows_per_tile) {}
   // steps of tiles 0 .. j - 1, and of tile j
   __host__ __device__ int64_t upto(int j) const { return (int64_t)j * base + (int64_t)each * ((int64_t)j * (j + 1) / 2); }
   __host__ __device__ int steps(int j) const { return base + each * (j + 1); }
@@ -132,7 +134,11 @@ struct CachePlan {
   CacheAttnArgs a;
   int workers;         // shares, at most
   CacheLeft* left;     // [workers]
-  float* partial;      // [workers][2][rows of a tile][hs + 2]: per row m, l, then O; [0]: the unit that began before the share
+  // [workers][2] partial results, [0]: of the unit that began before the share, [1]: of the one that goes on behind it.  Each: m and
+  // l of every row of a tile, then O.
+  float* partial;
+  int whole;           // shares end with units: there are no partial results
+  __host__ __device__ static int64_t slot(int rows_per_tile, int hs) { return (int64_t)rows_per_tile * (hs + 2); }
 };
 
 constexpr int kCacheRowsTile = 256;      // rows of a unit of the kernel for many rows

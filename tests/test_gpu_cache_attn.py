@@ -9,13 +9,16 @@ pytestmark = pytest.mark.gpu
 
 
 class Case:
-    def __init__(self, usp, seed, lens, news, hq, hk, hs, page, causal=True, o_dtype=sl.BF16, drop=0.0, strided=False, tail=0):
+    def __init__(self, usp, seed, lens, news, hq, hk, hs, page, causal=True, o_dtype=sl.BF16, drop=0.0, strided=False, tail=0, wide=False):
         rng = np.random.default_rng(seed)
         self.usp, self.hq, self.page, self.causal, self.o_dtype = usp, hq, page, causal, o_dtype
         self.lens, self.cu = np.asarray(lens), np.concatenate([[0], np.cumsum(news)])
         pages = sum(-(-max(x, 0) // page) for x in lens) + 2
         self.cache = sl.Cache(usp, rng, pages, page, hk, hs)
         self.table = sl.ragged_table(rng, [max(x, 0) for x in lens], page, pages, max(1, max(-(-max(x, 0) // page) for x in lens)))
+        if wide:        # room for more than 4096 tokens: units are cut between workgroups
+            more = np.full((len(lens), 4096 // page + 1), 0x7fffff02, dtype=np.int32)
+            self.table = np.concatenate([self.table, more], 1)
         if drop:
             self.table[rng.random(self.table.shape) < drop] = -1
         self.total = int(self.cu[-1]) + tail
@@ -55,9 +58,21 @@ HEADS = [(32, 8), (4, 4), (8, 1), (6, 2), (71, 1)]
 
 @pytest.mark.parametrize("hs,page", [(128, 64), (128, 16), (64, 32), (64, 128)])
 @pytest.mark.parametrize("hq,hk", HEADS)
-def test_single_tokens(usp, hs, page, hq, hk):
+@pytest.mark.parametrize("wide", [False, True])
+def test_single_tokens(usp, hs, page, hq, hk, wide):
     lens = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 500, 1003, 0]
-    Case(usp, hq + hs + page, lens, [1] * len(lens), hq, hk, hs, page).check()
+    Case(usp, hq + hs + page, lens, [1] * len(lens), hq, hk, hs, page, wide=wide).check()
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 5, 8, 13, 40, 300, 700])
+@pytest.mark.parametrize("wide", [False, True])
+def test_one_unit_cut_among_waves_and_workgroups(usp, steps, wide):
+    """One KV head and few steps or many: shares of none, one and several steps to a wave, with whole units between cut ones."""
+    if wide or steps <= 64:
+        Case(usp, steps, [64 * steps - 5], [1], 4, 1, 128, 64, wide=wide).check()
+    lens = [64 * steps, 1, 100, 64 * steps - 63, 64, 65]
+    if wide or steps <= 64:
+        Case(usp, steps + 1, lens, [1, 1, 2, 1, 1, 0], 4, 2, 64, 32, wide=wide).check()
 
 
 @pytest.mark.parametrize("hs,page,length", [(128, 64, 40000), (64, 16, 70001), (128, 128, 9999)])
@@ -69,11 +84,13 @@ def test_one_long_request(usp, hs, page, length, o_dtype):
 @pytest.mark.parametrize("hs,page", [(128, 64), (64, 16), (128, 32)])
 @pytest.mark.parametrize("hq,hk", [(32, 8), (4, 4), (6, 2), (8, 1)])
 @pytest.mark.parametrize("causal", [True, False])
-def test_ragged_rows(usp, hs, page, hq, hk, causal):
+@pytest.mark.parametrize("most", [1, 1000])
+def test_ragged_rows(usp, hs, page, hq, hk, causal, most):
     """No row, one and many; fewer keys than rows (rows that see nothing); lengths of zero; rows behind the last request."""
     news = [1, 0, 3, 8, 17, 40, 64, 5, 130]
     lens = [77, 50, 3, 5, 17, 700, 64, 0, 1000]
-    Case(usp, hq * hs + causal, lens, news, hq, hk, hs, page, causal=causal, strided=True, tail=3).check()
+    for wide in (False, True):          # (most: whether the kernel for few rows or the one for many has them)
+        Case(usp, hq * hs + causal, lens, news, hq, hk, hs, page, causal=causal, strided=True, tail=3, wide=wide).check(max_q=most)
 
 
 @pytest.mark.parametrize("hs", [64, 128])
@@ -93,7 +110,9 @@ def test_a_piece_of_a_prompt(usp, hs):
 def test_many_requests(usp, n):
     rng = np.random.default_rng(n)
     lens = np.where(rng.random(n) < 0.1, 0, np.exp(rng.uniform(0, 6.5, n)).astype(int))
-    Case(usp, n, lens.tolist(), rng.choice([0, 1, 1, 1, 2], n).tolist(), 4, 2, 64, 16).check()
+    for wide in (False, True):
+        for most in (2, 100):
+            Case(usp, n, lens.tolist(), rng.choice([0, 1, 1, 1, 2], n).tolist(), 4, 2, 64, 16, wide=wide).check(max_q=most)
 
 
 def test_the_most_rows_are_a_hint(usp):
