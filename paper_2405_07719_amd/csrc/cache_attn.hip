@@ -4,8 +4,8 @@
 // V share one read of them); its keys are walked in steps of 64.  All steps of all units, laid one behind the other, are cut
 // evenly among one workgroup per CU, and a workgroup's share among its eight waves, whatever the lengths: every workgroup works
 // out from the lengths, which stand on the device, where its share begins.  A unit that lies within one wave's share is finished
-// there.  Of one that is cut, the wave that has its beginning keeps its result (maximum, sum, unnormalised output) in
-// registers, the waves behind it put theirs into LDS, and the first adds them up in the order of the keys.  Units cut between
+// there.  The waves that share one put their results (maximum, sum, unnormalised output) into LDS, where all threads
+// add them up, each for a row and four columns, in the order of the keys.  Units cut between
 // workgroups leave partial results to a joining launch, two to a workgroup at most: the end of a unit that began before its share,
 // and the beginning of one that goes on behind it.
 //
@@ -79,7 +79,8 @@ struct Walk {
   int rows, token, hq;         // rows of the tile; the lane's row: its token (of all) and query head
 
   // Steps [s0, s1) of a unit.
-  __device__ __forceinline__ void unit(const CacheUnits& u, int seq, int head, int tile, int s0, int s1) {
+  template <typename Units>
+  __device__ __forceinline__ void unit(const Units& u, int seq, int head, int tile, int s0, int s1) {
     const CacheAttnArgs& a = p.a;
     const int32_t* const row = a.block_table + (int64_t)seq * a.max_pages;
     rows = u.rows(a, tile, kTile);
@@ -167,7 +168,7 @@ struct Walk {
         for (int e = 0; e < ET; ++e)
 #pragma unroll
           for (int w = 0; w < 4; ++w) any |= nan_codes(v[e][w]);
-        if (__ballot(any != 0)) {
+        if (__builtin_expect(__ballot(any != 0) != 0, 0)) {
           bf16x8 sees[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j)
@@ -217,94 +218,118 @@ struct Walk {
     }
     if (g == 0) a.lse[(int64_t)hq * a.total_q + token] = natural_lse(m, l);
   }
-  __device__ void put(float* slot, int row) const {
+  __device__ void put(float* slot) const {
     if (c >= rows) return;
     if (g == 0) ((f32x2*)slot)[c] = f32x2{m, l};
 #pragma unroll
-    for (int e = 0; e < ET; ++e) *(f32x4*)(slot + 2 * kTile + c * row + e * 16 + g * 4) = o[e];
+    for (int e = 0; e < ET; ++e) *(f32x4*)(slot + 2 * kTile + c * kLdsRow + e * 16 + g * 4) = o[e];
   }
-  // what the next wave has of the same unit
-  __device__ void add(const float* slot) {
-    if (c >= rows) return;
-    const f32x2 other = ((const f32x2*)slot)[c];
-    const float top = fmaxf(m, other[0]), use = top == -INFINITY ? 0.0f : top;
-    const float keep = exp2f(m - use), take = exp2f(other[0] - use);
-    l = l * keep + other[1] * take;
+};
+
+// Two partial results of a row as one.
+struct Sum {
+  float m, l;
+  f32x4 o;
+  __device__ void add(float m2, float l2, f32x4 o2) {
+    const float top = fmaxf(m, m2), use = top == -INFINITY ? 0.0f : top, keep = exp2f(m - use), take = exp2f(m2 - use);
     m = top;
-#pragma unroll
-    for (int e = 0; e < ET; ++e) o[e] = o[e] * keep + *(const f32x4*)(slot + 2 * kTile + c * kLdsRow + e * 16 + g * 4) * take;
+    l = l * keep + l2 * take;
+    o = o * keep + o2 * take;
+  }
+  // row `row` (of a tile's) of a unit, columns e .. e + 3
+  template <int HS, typename Units>
+  __device__ void write(const CacheAttnArgs& a, const Units& u, int head, int64_t row, int e) const {
+    const int in = (int)(row / a.group), hq = head * a.group + (int)(row - (int64_t)in * a.group), token = u.cu + in;
+    const f32x4 y = o * (l == 0.0f ? 0.0f : 1.0f / l);
+    const int64_t to = ((int64_t)token * (a.hk * a.group) + hq) * HS + e;
+    if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to) = __builtin_convertvector(y, bf16x4);
+    else *(f32x4*)((float*)a.o + to) = y;
+    if (e == 0) a.lse[(int64_t)hq * a.total_q + token] = natural_lse(m, l);
   }
 };
 
-template <int HS> struct Lds {
-  alignas(16) float slot[kWaves][Walk<HS>::kLdsSlot];
-  int first[kWaves];              // as in CacheLeft, of a wave's share
-  Shares<kThreads> shares;
+template <int HS, typename I> struct Lds {
+  alignas(16) float slot[2 * kWaves][Walk<HS>::kLdsSlot];     // of each wave: the end of a unit, the beginning of one
+  int first[kWaves];                                          // as in CacheLeft, of a wave's share
+  CacheLeft end[kWaves];
+  Shares<kThreads, I> shares;
 };
 
-template <int HS>
+template <int HS, typename I>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
   extern __shared__ __attribute__((aligned(16))) char dynamic[];
-  Lds<HS>& lds = *(Lds<HS>*)dynamic;
-  const Shares<kThreads>& shares = lds.shares;
-  const int64_t all = lds.shares.count(p.a, kTile);
+  Lds<HS, I>& lds = *(Lds<HS, I>*)dynamic;
+  const Shares<kThreads, I>& shares = lds.shares;
+  const I all = lds.shares.count(p.a, kTile);
   const int share = (int)blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int workers = all < p.workers ? (int)all : p.workers;
-  int64_t pos = share < workers ? all * share / workers : all, stop = share < workers ? all * (share + 1) / workers : all;
+  I pos = share < workers ? shares.cut(all, share, workers) : all, stop = share < workers ? shares.cut(all, share + 1, workers) : all;
   if (p.whole) {
     pos = shares.unit_start(p.a, kTile, pos, all);
     stop = shares.unit_start(p.a, kTile, stop, all);
   }
   // (rounded up: the first wave has a step wherever the workgroup has one)
-  const int64_t mine = pos + ((stop - pos) * wave + kWaves - 1) / kWaves, next = pos + ((stop - pos) * (wave + 1) + kWaves - 1) / kWaves;
+  const I n = stop - pos, mine = pos + n / kWaves * wave + (n % kWaves * wave + kWaves - 1) / kWaves,
+          next = pos + n / kWaves * (wave + 1) + (n % kWaves * (wave + 1) + kWaves - 1) / kWaves;
   Walk<HS> walk(p, threadIdx.x & 63);
-  float* const slots = p.partial + share * 2 * CachePlan::slot(kTile, HS);
-  int first = 0, end_seq = -1, end_head = 0, end_tile = 0;      // as in CacheLeft, of the wave's share
-  shares.walk(p.a, kTile, mine, next, [&](const CacheUnits& u, int seq, const CacheUnits::Place& at, int end, int of) __attribute__((always_inline)) {
-    const bool begins = at.step == 0, ends = end == of;
-    walk.unit(u, seq, at.head, at.tile, at.step, end);
+  int first = 0;
+  CacheLeft end = {0, -1, 0, 0};
+  shares.walk(p.a, kTile, mine, next, [&](const CacheUnits<I>& u, int seq, int head, int tile, int s0, int s1, int of) __attribute__((always_inline)) {
+    const bool begins = s0 == 0, ends = s1 == of;
+    walk.unit(u, seq, head, tile, s0, s1);
     if (begins && ends) {
       walk.write();
-    } else if (begins) {
-      end_seq = seq;
-      end_head = at.head;
-      end_tile = at.tile;
     } else {
-      first = ends ? 2 : 1;
-      if (wave) walk.put(lds.slot[wave], Walk<HS>::kLdsRow);
-      else if (ends) walk.put(slots, HS);
+      walk.put(lds.slot[2 * wave + begins]);
+      if (begins) end = CacheLeft{0, seq, head, tile};
+      else first = ends ? 2 : 1;
     }
   });
   // A wave without steps lets the unit that goes on around it pass (it has no partial result: 3).
-  if ((threadIdx.x & 63) == 0) lds.first[wave] = mine < next ? first : 3;
+  if ((threadIdx.x & 63) == 0) {
+    lds.first[wave] = mine < next ? first : 3;
+    lds.end[wave] = end;
+  }
   __syncthreads();
-  // The wave that has the beginning of a unit, or the workgroup's first part of one that began before, adds up what follows.
-  CacheLeft left = {wave == 0 ? first : 0, -1, 0, 0};
-  if (end_seq >= 0 || (wave == 0 && first == 1)) {
-    bool ended = false;
-    for (int w = wave + 1; w < kWaves && !ended; ++w) {
-      const int f = lds.first[w];
-      if (f == 1 || f == 2) walk.add(lds.slot[w]);
-      ended = f == 2;
-    }
-    if (end_seq < 0) {
-      walk.put(slots, HS);
-      left.first = ended ? 2 : 1;
-    } else if (ended) {
-      walk.write();
-    } else {
-      walk.put(slots + CachePlan::slot(kTile, HS), HS);
-      left.seq = end_seq, left.head = end_head, left.tile = end_tile;
+  // Units that waves share, each from the wave that has its beginning, or from the first wave, where the unit began in a workgroup
+  // before.
+  constexpr int kTeam = HS / 4;
+  const int row = threadIdx.x / kTeam, e = threadIdx.x % kTeam * 4;
+  CacheLeft left = {0, -1, 0, 0};
+  float* const slots = p.partial + share * 2 * CachePlan::slot(kTile, HS);
+  for (int w = 0; w < kWaves; ++w) {
+    const int f = lds.first[w];
+    for (int begins = w ? 1 : 0; begins < 2; ++begins) {
+      if (begins ? lds.end[w].seq < 0 : f != 1 && f != 2) continue;
+      bool ended = !begins && f == 2;
+      Sum sum = {-INFINITY, 0.0f, {0, 0, 0, 0}};
+      for (int x = w; ; ++x) {
+        if (x > w) {
+          if (ended || x == kWaves) break;
+          if (lds.first[x] == 3) continue;
+          ended = lds.first[x] == 2;
+        }
+        const float* const slot = lds.slot[2 * x + (x == w ? begins : 0)];
+        const f32x2 ml = ((const f32x2*)slot)[row & (kTile - 1)];
+        const f32x4 o = *(const f32x4*)(slot + 2 * kTile + (row & (kTile - 1)) * Walk<HS>::kLdsRow + e);
+        if (x == w) sum = Sum{ml[0], ml[1], o};
+        else sum.add(ml[0], ml[1], o);
+      }
+      if (begins && ended) {
+        const CacheUnits<I> u = shares.units(p.a, lds.end[w].seq, kTile);
+        if (row < u.rows(p.a, lds.end[w].tile, kTile)) sum.template write<HS>(p.a, u, lds.end[w].head, (int64_t)lds.end[w].tile * kTile + row, e);
+      } else {
+        float* const to = slots + (begins ? CachePlan::slot(kTile, HS) : 0);
+        if (row < kTile) {
+          if (e == 0) ((f32x2*)to)[row] = f32x2{sum.m, sum.l};
+          *(f32x4*)(to + 2 * kTile + row * HS + e) = sum.o;
+        }
+        if (begins) left.seq = lds.end[w].seq, left.head = lds.end[w].head, left.tile = lds.end[w].tile;
+        else left.first = ended ? 2 : 1;
+      }
     }
   }
-  if (p.whole) return;
-  // (one wave writes both parts of what the workgroup leaves: the last beginning may be any wave's)
-  __shared__ CacheLeft ends;
-  if (threadIdx.x == 0) ends.seq = -1;
-  __syncthreads();
-  if (left.seq >= 0 && (threadIdx.x & 63) == 0) ends = left;
-  __syncthreads();
-  if (threadIdx.x == 0) p.left[share] = CacheLeft{left.first, ends.seq, ends.head, ends.tile};
+  if (!p.whole && threadIdx.x == 0) p.left[share] = left;
 }
 
 // Joins the partial results of one unit: the beginning that worker w left, then what the workers behind it left up to the unit's
@@ -314,6 +339,7 @@ template <int HS>
 __global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan p, int rows_per_tile) {
   constexpr int kTeam = HS / 4, kTeams = kJoinThreads / kTeam;
   __shared__ f32x4 sums[kTeams][kTeam];
+  __shared__ f32x2 mls[kTeams];
   const int64_t slot = CachePlan::slot(rows_per_tile, HS);
   const CacheAttnArgs& a = p.a;
   const int w = blockIdx.x, lane = threadIdx.x & 63, team = threadIdx.x / kTeam, e = threadIdx.x % kTeam * 4;
@@ -330,48 +356,28 @@ __global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan
     parts += 64;
   }
   parts += w + parts < p.workers;                    // the one in which it ends
-  const CacheUnits u(a, mine.seq, rows_per_tile);
+  const CacheUnits<> u(a, mine.seq, rows_per_tile);
   const int rows = u.rows(a, mine.tile, rows_per_tile);
   const bool shared = parts >= kTeams;               // many parts to a row
   const auto slot_of = [&](int x) { return p.partial + (x ? 2 * (int64_t)(w + x) : 2 * (int64_t)w + 1) * slot; };
   const int step = shared ? gridDim.y : gridDim.y * kTeams;
   for (int row = shared ? blockIdx.y : blockIdx.y * kTeams + team; row < rows; row += step) {
-    float m = -INFINITY, l = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
+    Sum sum = {-INFINITY, 0.0f, {0, 0, 0, 0}};
 #pragma unroll 4
     for (int x = shared ? team : 0; x < parts; x += shared ? kTeams : 1) {
       const float* const at = slot_of(x);
       const f32x2 ml = ((const f32x2*)at)[row];
-      const f32x4 ox = *(const f32x4*)(at + 2 * rows_per_tile + row * HS + e);
-      const float top = fmaxf(m, ml[0]), use = top == -INFINITY ? 0.0f : top;
-      const float keep = exp2f(m - use), add = exp2f(ml[0] - use);
-      l = l * keep + ml[1] * add;
-      o = o * keep + ox * add;
-      m = top;
+      sum.add(ml[0], ml[1], *(const f32x4*)(at + 2 * rows_per_tile + row * HS + e));
     }
     if (shared) {                                    // the teams' sums, in their order
-      __shared__ f32x2 mls[kTeams];
       __syncthreads();
-      sums[team][threadIdx.x % kTeam] = o;
-      if (e == 0) mls[team] = f32x2{m, l};
+      sums[team][threadIdx.x % kTeam] = sum.o;
+      if (e == 0) mls[team] = f32x2{sum.m, sum.l};
       __syncthreads();
       if (team) continue;
-      for (int t = 1; t < kTeams; ++t) {
-        const f32x2 ml = mls[t];
-        const float top = fmaxf(m, ml[0]), use = top == -INFINITY ? 0.0f : top;
-        const float keep = exp2f(m - use), add = exp2f(ml[0] - use);
-        l = l * keep + ml[1] * add;
-        o = o * keep + sums[t][threadIdx.x] * add;
-        m = top;
-      }
+      for (int t = 1; t < kTeams; ++t) sum.add(mls[t][0], mls[t][1], sums[t][threadIdx.x]);
     }
-    const int64_t row_in = (int64_t)mine.tile * rows_per_tile + row;
-    const int token = (int)(row_in / a.group), h = mine.head * a.group + (int)(row_in - (int64_t)token * a.group);
-    const f32x4 y = o * (l == 0.0f ? 0.0f : 1.0f / l);
-    const int64_t to = ((int64_t)(u.cu + token) * (a.hk * a.group) + h) * HS + e;
-    if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to) = __builtin_convertvector(y, bf16x4);
-    else *(f32x4*)((float*)a.o + to) = y;
-    if (e == 0) a.lse[(int64_t)h * a.total_q + u.cu + token] = natural_lse(m, l);
+    sum.template write<HS>(a, u, mine.head, (int64_t)mine.tile * rows_per_tile + row, e);
   }
 }
 
@@ -380,12 +386,19 @@ __global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan
 bool few_rows(int group, int max_q) { return (int64_t)group * (max_q < 1 ? 1 : max_q) <= 16; }
 int rows_of(bool few) { return few ? kTile : kCacheRowsTile; }
 
-template <int HS>
+template <int HS, typename I>
 int launch_few(const CachePlan& p, hipStream_t stream) {
   static LdsLimitRaised raised;
-  if (!raise_dynamic_lds_limit((const void*)cache_attn_kernel<HS>, sizeof(Lds<HS>), raised)) return USP_ERR_LAUNCH;
-  cache_attn_kernel<HS><<<dim3(p.workers), kThreads, sizeof(Lds<HS>), stream>>>(p);
+  if (!raise_dynamic_lds_limit((const void*)cache_attn_kernel<HS, I>, sizeof(Lds<HS, I>), raised)) return USP_ERR_LAUNCH;
+  cache_attn_kernel<HS, I><<<dim3(p.workers), kThreads, sizeof(Lds<HS, I>), stream>>>(p);
   return USP_OK;
+}
+template <int HS>
+int launch_few(const CachePlan& p, hipStream_t stream) {
+  const CacheAttnArgs& a = p.a;
+  // steps that there can be: tiles, each of the steps of a full table and of one more for each tile before it
+  const double tiles = (double)a.total_q * a.group / kTile + a.n_seqs, steps = (double)((int64_t)a.max_pages << a.page_shift) / kStep + 2 + tiles;
+  return tiles * steps * a.hk < 2e9 ? launch_few<HS, int32_t>(p, stream) : launch_few<HS, int64_t>(p, stream);
 }
 
 }  // namespace
@@ -398,9 +411,9 @@ int launch_cache_attn(const CacheAttnArgs& a, int max_q, hipStream_t stream) {
   const bool few = few_rows(a.group, max_q);
   CachePlan p = {a, kPlanCUs, (CacheLeft*)a.workspace, nullptr, 0};
   p.partial = (float*)(p.left + p.workers);
-  // Rows of the table that hold 4096 tokens at most: a wave has eight steps of a unit at most, and the joining launch would cost
-  // more than cutting units between workgroups gains.
-  p.whole = few && (int64_t)a.max_pages << a.page_shift <= 4096;
+  // Rows of the table that hold 4096 tokens at most, and a unit and more for every CU: a wave has eight steps of a unit at most, and
+  // the joining launch would cost more than cutting units between workgroups gains.
+  p.whole = few && (int64_t)a.max_pages << a.page_shift <= 4096 && (int64_t)a.n_seqs * a.hk >= kPlanCUs;
   const int st = !few ? launch_cache_attn_rows(p, stream) : a.hs == 128 ? launch_few<128>(p, stream) : launch_few<64>(p, stream);
   if (st != USP_OK) return st;
   if (!p.whole) {

@@ -33,26 +33,27 @@ __device__ inline uint32_t first_bytes(int n) { return n >= 4 ? 0xffffffffu : n 
 
 __device__ inline float natural_lse(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f; }
 
-// The steps of all requests' units, laid one behind the other and cut into shares.
-template <int THREADS>
+// The steps of all requests' units, laid one behind the other and cut into shares.  I: as in CacheUnits.
+template <int THREADS, typename I>
 struct Shares {
-  int64_t before[THREADS + 1];     // steps of the requests before a thread's first one
-  int64_t part[THREADS / 64];
-  CacheUnits::Request first[THREADS];   // each thread's first request
+  typedef CacheUnits<I> Units;
+  I before[THREADS + 1];           // steps of the requests before a thread's first one
+  I part[THREADS / 64];
+  CacheRequest first[THREADS];     // each thread's first request
 
   // By all threads of a workgroup: the steps in all.  Each thread counts `n / THREADS` requests in a row.
-  __device__ int64_t count(const CacheAttnArgs& a, int rows_per_tile) {
+  __device__ I count(const CacheAttnArgs& a, int rows_per_tile) {
     const int tid = threadIdx.x, lane = tid & 63, n = a.n_seqs, per = (n + THREADS - 1) / THREADS;
-    int64_t sum = 0;
+    I sum = 0;
     for (int i = tid * per; i < (tid + 1) * per && i < n; ++i) {
-      const CacheUnits::Request r = CacheUnits::read(a, i);
+      const CacheRequest r = Units::read(a, i);
       if (i == tid * per) first[tid] = r;
-      sum += CacheUnits(a, r, rows_per_tile).per_head * a.hk;
+      sum += Units(a, r, rows_per_tile).per_head * a.hk;
     }
-    int64_t upto = sum, all = 0;
+    I upto = sum, all = 0;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-      const int64_t x = __shfl_up(upto, d);
+      const I x = __shfl_up(upto, d);
       if (lane >= d) upto += x;
     }
     if (lane == 63) part[tid >> 6] = upto;
@@ -68,22 +69,27 @@ struct Shares {
     return all;
   }
 
-  __device__ CacheUnits units(const CacheAttnArgs& a, int seq, int rows_per_tile) const {
-    return a.n_seqs <= THREADS ? CacheUnits(a, first[seq], rows_per_tile) : CacheUnits(a, seq, rows_per_tile);
+  // Where share `i` of `n` begins.
+  __device__ static I cut(I all, int i, int n) {
+    const I q = all / n, r = all - q * n;          // (r * i stays small)
+    return q * i + r * i / n;
   }
 
-  struct Where { int seq; int64_t start; };      // a request, and its first step
-  __device__ __forceinline__ Where find(const CacheAttnArgs& a, int rows_per_tile, int64_t pos) const {
-    const int per = (a.n_seqs + THREADS - 1) / THREADS;
-    int lo = 0, hi = THREADS;                    // the last thread whose first request begins at pos or before
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (before[mid] <= pos) lo = mid;
-      else hi = mid;
-    }
-    Where w = {__builtin_amdgcn_readfirstlane(lo * per), before[lo]};
+  __device__ Units units(const CacheAttnArgs& a, int seq, int rows_per_tile) const {
+    return a.n_seqs <= THREADS ? Units(a, first[seq], rows_per_tile) : Units(a, seq, rows_per_tile);
+  }
+
+  struct Where { int seq; I start; };      // a request, and its first step
+  __device__ __forceinline__ Where find(const CacheAttnArgs& a, int rows_per_tile, I pos) const {
+    // The last thread whose first request begins at pos or before, by 64 samples and then between two of them.
+    constexpr int kEach = THREADS / 64;
+    const int lane = threadIdx.x & 63, per = (a.n_seqs + THREADS - 1) / THREADS;
+    int t = (63 - __builtin_clzll(__ballot(before[lane * kEach] <= pos))) * kEach;
+    t += 63 - __builtin_clzll(__ballot(lane < kEach && before[t + (lane & (kEach - 1))] <= pos));
+    t = __builtin_amdgcn_readfirstlane(t);
+    Where w = {t * per, before[t]};
     for (; per > 1 && w.seq < a.n_seqs; ++w.seq) {
-      const int64_t steps = units(a, w.seq, rows_per_tile).per_head * a.hk;
+      const I steps = units(a, w.seq, rows_per_tile).per_head * a.hk;
       if (pos < w.start + steps) break;
       w.start += steps;
     }
@@ -91,7 +97,7 @@ struct Shares {
   }
 
   // The first step of the unit that step `pos` is of (the last step of all and one: itself).
-  __device__ __forceinline__ int64_t unit_start(const CacheAttnArgs& a, int rows_per_tile, int64_t pos, int64_t all) const {
+  __device__ __forceinline__ I unit_start(const CacheAttnArgs& a, int rows_per_tile, I pos, I all) const {
     if (pos >= all) return all;
     const Where w = find(a, rows_per_tile, pos);
     return pos - units(a, w.seq, rows_per_tile).locate(pos - w.start).step;
@@ -99,20 +105,20 @@ struct Shares {
 
   // The pieces of units that steps [pos, stop) are, one after the other: visit(units, seq, place, end step, whole unit's steps).
   template <class Visit>
-  __device__ __forceinline__ void walk(const CacheAttnArgs& a, int rows_per_tile, int64_t pos, int64_t stop, Visit visit) const {
+  __device__ __forceinline__ void walk(const CacheAttnArgs& a, int rows_per_tile, I pos, I stop, Visit visit) const {
     if (pos >= stop) return;
     Where w = find(a, rows_per_tile, pos);
     while (pos < stop && w.seq < a.n_seqs) {
-      const CacheUnits u = units(a, w.seq, rows_per_tile);
-      const int64_t steps = u.per_head * a.hk;
+      const Units u = units(a, w.seq, rows_per_tile);
+      const I steps = u.per_head * a.hk;
       if (pos >= w.start + steps) {
         w.start += steps;
         ++w.seq;
         continue;
       }
-      const CacheUnits::Place at = u.locate(pos - w.start);
+      const typename Units::Place at = u.locate(pos - w.start);
       const int of = u.steps(at.tile), end = stop - pos < of - at.step ? at.step + (int)(stop - pos) : of;
-      visit(u, w.seq, at, end, of);
+      visit(u, w.seq, at.head, at.tile, at.step, end, of);
       pos += end - at.step;
     }
   }

@@ -32,7 +32,7 @@ template <int HS> struct Lds {
   alignas(16) char v[2][v_bytes<HS>()];
   alignas(16) Marks marks[2];
   alignas(8) uint16_t nan[2][HS][4];
-  Shares<kThreads> shares;
+  Shares<kThreads, int64_t> shares;
 };
 
 template <int HS>
@@ -187,7 +187,7 @@ struct RowsWalk {
   }
 
   // Steps [s0, s1) of a unit: results to o and lse if these are all, else to the partial result `slot`.
-  __device__ __forceinline__ void unit(const CacheUnits& u, int seq, int head, int tile, int s0, int s1, bool whole, float* slot) {
+  __device__ __forceinline__ void unit(const CacheUnits<>& u, int seq, int head, int tile, int s0, int s1, bool whole, float* slot) {
     const int32_t* const row = a.block_table + (int64_t)seq * a.max_pages;
     const int rows = u.rows(a, tile, kCacheRowsTile);
     const int64_t row_first = (int64_t)tile * kCacheRowsTile;
@@ -277,7 +277,7 @@ template <int HS>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(CachePlan p) {
   extern __shared__ __attribute__((aligned(16))) char dynamic[];
   Lds<HS>& shared = *(Lds<HS>*)dynamic;
-  const Shares<kThreads>& shares = shared.shares;
+  const Shares<kThreads, int64_t>& shares = shared.shares;
   const int64_t all = shared.shares.count(p.a, kCacheRowsTile);
   // The workgroups of an XCD (blockIdx % 8) have shares that follow on one another: mostly of one KV head.
   const int n = (int)gridDim.x, share = n % 8 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (n / 8) + (int)blockIdx.x / 8;
@@ -286,12 +286,12 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(CachePlan 
   if (share < workers) {
     RowsWalk<HS> walk(p.a, shared);
     float* const slots = p.partial + share * 2 * CachePlan::slot(kCacheRowsTile, HS);
-    shares.walk(p.a, kCacheRowsTile, all * share / workers, all * (share + 1) / workers,
-                [&](const CacheUnits& u, int seq, const CacheUnits::Place& at, int end, int of) __attribute__((always_inline)) {
-                  const bool begins = at.step == 0, ends = end == of;
-                  walk.unit(u, seq, at.head, at.tile, at.step, end, begins && ends, slots + (begins ? CachePlan::slot(kCacheRowsTile, HS) : 0));
+    shares.walk(p.a, kCacheRowsTile, shares.cut(all, share, workers), shares.cut(all, share + 1, workers),
+                [&](const CacheUnits<>& u, int seq, int head, int tile, int s0, int end, int of) __attribute__((always_inline)) {
+                  const bool begins = s0 == 0, ends = end == of;
+                  walk.unit(u, seq, head, tile, s0, end, begins && ends, slots + (begins ? CachePlan::slot(kCacheRowsTile, HS) : 0));
                   if (!begins) left.first = ends ? 2 : 1;
-                  else if (!ends) left.seq = seq, left.head = at.head, left.tile = at.tile;
+                  else if (!ends) left.seq = seq, left.head = head, left.tile = tile;
                 });
   }
   if (threadIdx.x == 0) p.left[share] = left;

@@ -61,12 +61,16 @@ struct CacheAttnArgs {
 // Keys of one step of a unit's walk.
 constexpr int kCacheStep = 64;
 
+struct CacheRequest { int cu, nq, len; };      // first row, rows, keys
+
 // One request's units (KV head, tile of rows) and how many steps each is taken to have: tiles of a causal request see more keys
 // one after the other.  (Exact for a single tile, else up to a step too many; a tile that is at its end early is done early.)
+// I: what holds sums of steps; 32 bits where they cannot be more (divisions of 64 bits are long).
+template <typename I = int64_t>
 struct CacheUnits {
   int cu, nq, len, tiles, base, each, causal;
-  int64_t per_head;   // steps of one KV head's tiles
-  struct Request { int cu, nq, len; };      // first row, rows, keys
+  I per_head;   // steps of one KV head's tiles
+  typedef CacheRequest Request;
   __host__ __device__ static Request read(const CacheAttnArgs& a, int i) {
     const int total = (int)a.total_q;
     int c0 = a.cu_q[i], c1 = a.cu_q[i + 1];
@@ -88,7 +92,7 @@ struct CacheUnits {
   }
   __host__ __device__ CacheUnits(const CacheAttnArgs& a, int i, int rows_per_tile) : CacheUnits(a, read(a, i), rows_per_tile) {}
   // steps of tiles 0 .. j - 1, and of tile j
-  __host__ __device__ int64_t upto(int j) const { return (int64_t)j * base + (int64_t)each * ((int64_t)j * (j + 1) / 2); }
+  __host__ __device__ I upto(int j) const { return (I)j * base + (I)each * (I)((int64_t)j * (j + 1) / 2); }
   __host__ __device__ int steps(int j) const { return base + each * (j + 1); }
   // keys that a token sees
   __host__ __device__ int seen_by(int64_t token) const {
@@ -102,9 +106,9 @@ struct CacheUnits {
   }
   // the unit and its step at `pos` of the request's steps (head after head, tile after tile)
   struct Place { int head, tile, step; };
-  __host__ __device__ Place locate(int64_t pos) const {
+  __host__ __device__ Place locate(I pos) const {
     const int head = (int)(pos / per_head);
-    const int64_t in_head = pos - head * per_head;
+    const I in_head = pos - head * per_head;
     int tile = 0, above = tiles;
     while (above - tile > 1) {
       const int mid = (tile + above) / 2;

@@ -146,7 +146,7 @@ extern "C" int walk(const int32_t* cu, const int32_t* lens, int n, int64_t total
   a.n_seqs = n; a.causal = causal;
   int64_t all = 0;
   std::vector<int64_t> before(n + 1, 0);
-  for (int i = 0; i < n; ++i) before[i + 1] = all += CacheUnits(a, i, rt).per_head * hk;
+  for (int i = 0; i < n; ++i) before[i + 1] = all += CacheUnits<>(a, i, rt).per_head * hk;
   const int shares = all < waves ? (int)all : waves;
   int open = 0;      // a unit that began and is not at its end yet
   int seq = 0;
@@ -158,7 +158,7 @@ extern "C" int walk(const int32_t* cu, const int32_t* lens, int n, int64_t total
     int first = 0;
     while (pos < stop) {
       while (before[seq + 1] <= pos) ++seq;
-      const CacheUnits u(a, seq, rt);
+      const CacheUnits<> u(a, seq, rt);
       const auto at = u.locate(pos - before[seq]);
       const int of = u.steps(at.tile);
       if (at.head < 0 || at.head >= hk || at.tile < 0 || at.tile >= u.tiles || at.step < 0 || at.step >= of) return 2;
