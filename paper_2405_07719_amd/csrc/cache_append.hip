@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(CacheAppendArgs 
 int launch_cache_append(const CacheAppendArgs& args, int dtype, hipStream_t stream) {
   CacheAppendArgs a = args;
   // Rows in which a wave looks for pages that begin there.
-  a.window = a.rows <= 2048 ? 1 : 8;
+  a.window = a.rows <= 2048 ? 1 : a.rows <= USP_CACHE_MAX_REQUESTS ? 8 : 64;
   // (several launches where one would have 2^32 threads or more)
   const int64_t windows = (a.rows + a.window - 1) / a.window, most = max_workgroups(kThreads) * (kThreads / 64) / (2 * a.hk);
   for (a.first_window = 0; a.first_window < windows; a.first_window += most) {

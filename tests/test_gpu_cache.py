@@ -103,14 +103,14 @@ def test_append(usp, page, hs, dtype):
     append_case(usp, page, 1, hs, dtype, [5, 0], [page - 5, 3 * page + 7], 4, strided=True)
 
 
-@pytest.mark.parametrize("rows", [2048, 2049, 5000])
+@pytest.mark.parametrize("rows", [2048, 2049, 5000, 8192, 8200, 20000])
 def test_append_of_many_rows(usp, rows):
     """Waves that look at one row each, and at several."""
     rng = np.random.default_rng(rows)
     news = []
     while sum(news) < rows:
         news.append(int(min(rng.choice([1, 1, 2, 30, 130]), rows - sum(news))))
-    append_case(usp, 32, 2, 64, sl.BF16, rng.integers(0, 90, len(news)).tolist(), news, rows, spread=1.0)
+    append_case(usp, 32, 1, 64, sl.BF16, rng.integers(0, 90, len(news)).tolist(), news, rows, spread=1.0)
 
 
 @pytest.mark.parametrize("dtype", [sl.BF16, sl.FP32])
