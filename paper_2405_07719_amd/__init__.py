@@ -143,15 +143,20 @@ def _ptr(x):
     return x.data_ptr()
 
 
-def _here(x):
-    """_ptr of a tensor that lies on the current device: the launch goes to that device's stream, and an address of another
-    one, or of the host, would be a fault there."""
-    if x is None or isinstance(x, int):
-        return x
-    device = x.get_device()
-    if device < 0 or device != (_raw_device() if _raw_device is not None else device):
-        raise ValueError(f"a tensor on {x.device} given to a launch on the current HIP device")
-    return x.data_ptr()
+def _elsewhere(x):
+    raise ValueError(f"a tensor on {x.device} given to a launch on the current HIP device")
+
+
+def _here(*tensors):
+    """_ptr of tensors that lie on the current device: the launch goes to that device's stream, and an address of another one, or
+    of the host, would be a fault there."""
+    cuda = _torch_cuda
+    if cuda is not None and cuda.is_initialized():
+        device = _raw_device()
+    else:
+        import torch
+        device = torch.cuda.current_device() if torch.cuda.is_initialized() else None     # (None: no tensor is on a device)
+    return [x if x is None or type(x) is int else x.data_ptr() if x.get_device() == device else _elsewhere(x) for x in tensors]
 
 
 def _stream(stream):
@@ -358,32 +363,35 @@ def rope(hs, rotary_dim, layout, base, scaling=USP_ROPE_UNSCALED, factor=1.0, al
 
 
 def usp_rope_shards(p, r, q, k, q_out, k_out, backward, rank_begin, rank_end, stream=None):
-    _check(load().usp_rope_shards(C.byref(p), C.byref(r), _here(q), _here(k), _here(q_out), _here(k_out), int(bool(backward)),
-                                  rank_begin, rank_end, _stream(stream)), "usp_rope_shards")
+    _check((_lib or load()).usp_rope_shards(C.byref(p), C.byref(r), *_here(q, k, q_out, k_out), 1 if backward else 0, rank_begin,
+                                            rank_end, _stream(stream)), "usp_rope_shards")
 
 
 def usp_rope_rows(r, q, k, q_out, k_out, positions, rows, hq, hk, hs, q_stride, k_stride, q_out_stride, k_out_stride, dtype,
                   backward, stream=None):
-    _check(load().usp_rope_rows(C.byref(r), _here(q), _here(k), _here(q_out), _here(k_out), _here(positions), rows, hq, hk, hs,
-                                q_stride, k_stride, q_out_stride, k_out_stride, dtype, int(bool(backward)), _stream(stream)),
+    _check((_lib or load()).usp_rope_rows(C.byref(r), *_here(q, k, q_out, k_out, positions), rows, hq, hk, hs, q_stride, k_stride,
+                                          q_out_stride, k_out_stride, dtype, 1 if backward else 0, _stream(stream)),
            "usp_rope_rows")
 
 
 def cache(k_codes, v_codes, k_scale, v_scale, pages, page, hk, hs):
     """A usp_cache over the four tensors; it holds their addresses, not the tensors, which have to live as long as it is used."""
-    return usp_cache(_here(k_codes), _here(v_codes), _here(k_scale), _here(v_scale), pages, page, hk, hs, 0)
+    load()
+    return usp_cache(*_here(k_codes, v_codes, k_scale, v_scale), pages, page, hk, hs, 0)
 
 
 def usp_cache_extend(cu_new, len_before, n_seqs, total_new, block_table, max_pages, page, pages, free_pages, n_free, len_after,
                      slots, positions, taken, stream=None):
-    _check(load().usp_cache_extend(_here(cu_new), _here(len_before), n_seqs, total_new, _here(block_table), max_pages, page,
-                                   pages, _here(free_pages), n_free, _here(len_after), _here(slots), _here(positions),
-                                   _here(taken), _stream(stream)), "usp_cache_extend")
+    lib = _lib or load()
+    cu, before, table, free, after, slots, positions, taken = _here(cu_new, len_before, block_table, free_pages, len_after, slots,
+                                                                    positions, taken)
+    _check(lib.usp_cache_extend(cu, before, n_seqs, total_new, table, max_pages, page, pages, free, n_free, after, slots, positions,
+                                taken, _stream(stream)), "usp_cache_extend")
 
 
 def usp_cache_append(c, k, v, slots, rows, k_stride, v_stride, dtype, stream=None):
-    _check(load().usp_cache_append(C.byref(c), _here(k), _here(v), _here(slots), rows, k_stride, v_stride, dtype,
-                                   _stream(stream)), "usp_cache_append")
+    _check((_lib or load()).usp_cache_append(C.byref(c), *_here(k, v, slots), rows, k_stride, v_stride, dtype, _stream(stream)),
+           "usp_cache_append")
 
 
 def usp_cache_attn_workspace_bytes(c, hq, max_q):
@@ -394,6 +402,7 @@ def usp_cache_attn(c, q, q_stride, cu_q, kv_len, block_table, max_pages, n_seqs,
                    o_dtype, workspace, workspace_bytes=None, stream=None):
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    _check(load().usp_cache_attn(C.byref(c), _here(q), q_stride, _here(cu_q), _here(kv_len), _here(block_table), max_pages,
-                                 n_seqs, total_q, max_q, hq, scale, int(bool(causal)), _here(o), _here(lse), o_dtype,
-                                 _here(workspace), workspace_bytes, _stream(stream)), "usp_cache_attn")
+    lib = _lib or load()
+    q, cu, lens, table, o, lse, workspace = _here(q, cu_q, kv_len, block_table, o, lse, workspace)
+    _check(lib.usp_cache_attn(C.byref(c), q, q_stride, cu, lens, table, max_pages, n_seqs, total_q, max_q, hq, scale,
+                              1 if causal else 0, o, lse, o_dtype, workspace, workspace_bytes, _stream(stream)), "usp_cache_attn")

@@ -32,19 +32,20 @@ __device__ inline void sine_cosine(double turns, float* s, float* c) {
   *c = (quadrant + 1) & 2 ? -b : b;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int head_groups, int64_t first_row) {
+// 2^log_groups threads share a row's heads.
+template <typename T, int HS>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int log_groups, int64_t first_row) {
   typedef typename Vec<T>::type V;
   typedef typename Vec<T>::wide W;
-  constexpr int E = Vec<T>::E;
-  const int units = a.hs / (2 * E);                        // threads that hold one head of one row
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int unit = (int)(id % units);
-  const int64_t rest = id / units;
-  const int group = (int)(rest % head_groups);
-  const int64_t row = first_row + rest / head_groups;
+  constexpr int E = Vec<T>::E, kUnits = HS / (2 * E);      // threads that hold one head of one row
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x, unit = id % kUnits, rest = id / kUnits;
+  double turns_of[E];                                      // (ahead of all that waits for the other arguments)
+#pragma unroll
+  for (int e = 0; e < E; ++e) turns_of[e] = a.turns[unit * E + e];
+  const int group = (int)(rest & ((1u << log_groups) - 1)), head_groups = 1 << log_groups;
+  const int64_t row = first_row + (rest >> log_groups);
   if (row >= a.rows) return;
-  const bool turns = unit * 2 * E < a.rotary_dim;
+  const bool turns = (int)unit * 2 * E < a.rotary_dim;
   if (!turns && a.in_place) return;
   int64_t pos;
   if (a.positions) {
@@ -59,19 +60,19 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int head_gro
   float s[E], c[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    sine_cosine(turns ? (double)pos * a.turns[unit * E + e] : 0.0, &s[e], &c[e]);
+    sine_cosine((double)pos * turns_of[e], &s[e], &c[e]);
     s[e] *= a.sign * a.magnitude;
     c[e] *= a.magnitude;
   }
   // the first of each pair begins at element e0, the second (or the next E elements) at e1
   const bool halves = turns && !a.pairs;
-  const int e0 = halves ? unit * E : unit * 2 * E, e1 = halves ? e0 + a.rotary_dim / 2 : e0 + E;
+  const int e0 = (int)unit * (halves ? E : 2 * E), e1 = halves ? e0 + a.rotary_dim / 2 : e0 + E;
   const int heads = a.heads[0] + a.heads[1];
 #pragma unroll 2
   for (int h = group; h < heads; h += head_groups) {
     const int t = h >= a.heads[0], ht = t ? h - a.heads[0] : h;
-    const T* x = (const T*)a.x[t] + row * a.stride[t] + ht * a.hs;
-    T* y = (T*)a.y[t] + row * a.out_stride[t] + ht * a.hs;
+    const T* x = (const T*)a.x[t] + row * a.stride[t] + ht * HS;
+    T* y = (T*)a.y[t] + row * a.out_stride[t] + ht * HS;
     V va = *(const V*)(x + e0), vb = *(const V*)(x + e1);
     if (turns) {
       const W fa = __builtin_convertvector(va, W), fb = __builtin_convertvector(vb, W);
@@ -101,22 +102,25 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int head_gro
 
 }  // namespace
 
+template <typename T>
+static void launch(const RopeArgs& a, int log_groups, int64_t first, unsigned grid, hipStream_t stream) {
+  if (a.hs == 128) rope_kernel<T, 128><<<dim3(grid), kThreads, 0, stream>>>(a, log_groups, first);
+  else rope_kernel<T, 64><<<dim3(grid), kThreads, 0, stream>>>(a, log_groups, first);
+}
+
 int launch_rope(const RopeArgs& a, int dtype, hipStream_t stream) {
   const int heads = a.heads[0] + a.heads[1], units = a.hs / (dtype == USP_BF16 ? 16 : 8);
   // One thread per row, unit and head while that fills the chip once over; then more heads to a thread, which forms its
   // angles once for all of them.
-  int groups = 1;
-  while (groups < heads && a.rows * units * groups < (int64_t)kPlanCUs * 2048) groups *= 2;
-  groups = groups < heads ? groups : heads;
+  int log_groups = 0;
+  while (2 << log_groups <= heads && a.rows * units << log_groups < (int64_t)kPlanCUs * 2048) ++log_groups;
   // (several launches where one would have 2^32 threads or more)
-  const int64_t most = max_workgroups(kThreads) * kThreads / (units * groups);
+  const int64_t most = max_workgroups(kThreads) * kThreads / units >> log_groups;
   for (int64_t first = 0; first < a.rows; first += most) {
     const int64_t rows = a.rows - first < most ? a.rows - first : most;
-    const unsigned grid = (unsigned)((rows * units * groups + kThreads - 1) / kThreads);
-    if (dtype == USP_BF16)
-      rope_kernel<__bf16><<<dim3(grid), kThreads, 0, stream>>>(a, groups, first);
-    else
-      rope_kernel<float><<<dim3(grid), kThreads, 0, stream>>>(a, groups, first);
+    const unsigned grid = (unsigned)(((rows * units << log_groups) + kThreads - 1) / kThreads);
+    if (dtype == USP_BF16) launch<__bf16>(a, log_groups, first, grid, stream);
+    else launch<float>(a, log_groups, first, grid, stream);
   }
   return launch_status();
 }
