@@ -24,9 +24,9 @@ template <int HS> constexpr int k_stride() { return HS * 2 + 16; }
 constexpr int kVStride = kStep * 2 + 16;
 template <int HS> constexpr int k_bytes() { return kStep * k_stride<HS>(); }
 template <int HS> constexpr int v_bytes() { return HS * kVStride; }
-// Beside K and V, for each of the two buffers: which of a step's 16-token blocks have a page (a byte each), whether a wave brought
+// Beside K and V, for each of the two buffers: which of a step's 16-token blocks have no page (a byte each), whether a wave brought
 // NaN values (a byte each), and where they are (16 bits for each column and block).
-struct Marks { uint8_t there[4], unused[4], nan[kThreads / 64]; };
+struct Marks { uint8_t missing[4], unused[4], nan[kThreads / 64]; };
 template <int HS> struct Lds {
   alignas(16) char k[2][k_bytes<HS>()];
   alignas(16) char v[2][v_bytes<HS>()];
@@ -54,16 +54,21 @@ struct RowsWalk {
   __device__ bool brings_k() const { return kBoth || wave < 4; }
   __device__ bool brings_v() const { return kBoth || wave >= 4; }
 
+  // The wave's block of a step: where its page's scales and its own codes are, of K as of V, and how many of its tokens count.
   // (A page that is not there reads page 0, unconditionally: a load under a condition would be waited for where it stands.)
-  struct Piece { u32x4 codes; uint32_t scale; };
-  __device__ Piece load(const uint8_t* codes, const uint8_t* scales, int number, int step, int head) const {
-    const int64_t place = (int64_t)(number < 0 ? 0 : number) * a.hk + head;
-    const int inside = (step * kStep + block * 16) & ((1 << a.page_shift) - 1);
-    return Piece{*(const u32x4*)(codes + ((place << a.page_shift) + inside) * HS + piece * 16), scales[place]};
-  }
-  // The page of the wave's block of a step; blocks behind the last one that counts are taken for that one.
-  __device__ int find(const int32_t* row, int step, int vis) const {
+  struct Block { int64_t place, codes; int left; };
+  __device__ int number(const int32_t* row, int step, int vis) const {
     return __builtin_amdgcn_readfirstlane(row[cache_entry(step * 4 + block, vis, a.page_shift)]);
+  }
+  __device__ Block found(int number, int step, int vis, int head) const {
+    const bool counts = cache_counts(step * 4 + block, vis, number, a.pages);
+    const int inside = (step * kStep + block * 16) & ((1 << a.page_shift) - 1);
+    const int64_t place = (int64_t)(counts ? number : 0) * a.hk + head;
+    return Block{place, ((place << a.page_shift) + inside) * HS, counts ? vis - step * kStep - block * 16 : 0};
+  }
+  struct Piece { u32x4 codes; uint32_t scale; };
+  __device__ Piece load(const uint8_t* codes, const uint8_t* scales, const Block& b) const {
+    return Piece{*(const u32x4*)(codes + b.codes + piece * 16), scales[b.place]};
   }
 
   __device__ void put_k(const Piece& x, int buffer) const {
@@ -74,8 +79,9 @@ struct RowsWalk {
     to[1] = widened(x.codes[2], x.codes[3], scale);
   }
   // `left`: how many of the block's tokens count.  What stands behind them counts as zero, whatever it is; NaN, too, which is
-  // kept apart: 0 times it would be NaN for rows that do not see it.
-  __device__ void put_v(const Piece& x, int buffer, int left) const {
+  // kept apart: 0 times it would be NaN for rows that do not see it.  `marked`: the wave's marks in a buffer are not those of
+  // 16 tokens without NaN, which the kernel begins with.
+  __device__ void put_v(const Piece& x, int buffer, int left, int& marked) const {
     const float scale = left > 0 ? scale_of(x.scale) : 1.0f;      // (0 times the NaN of a page in no use would be NaN)
     u32x4 y = x.codes;
     if (left < 16) {
@@ -83,24 +89,30 @@ struct RowsWalk {
       for (int w = 0; w < 4; ++w) y[w] &= first_bytes(left - 4 * w);
     }
     const uint32_t any = nan_codes(y[0]) | nan_codes(y[1]) | nan_codes(y[2]) | nan_codes(y[3]);
-    const bool some = __ballot(any != 0) != 0;
-    uint32_t where = 0;
-    if (some) {
+    const bool some = __ballot(any != 0) != 0, mark = some || left <= 0;
+    if (__builtin_expect(mark || (marked >> buffer & 1), 0)) {
+      uint32_t where = 0;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const uint32_t n = nan_codes(y[w]) >> 7;
         where |= ((n | n >> 7 | n >> 14 | n >> 21) & 15) << (4 * w);
         y[w] &= ~(n * 0xff);
       }
+      lds.nan[buffer][piece][block] = (uint16_t)where;
+      if ((tid & 63) == 0) {
+        lds.marks[buffer].nan[wave] = some;
+        lds.marks[buffer].missing[block] = left <= 0;
+      }
+      marked = (marked & ~(1 << buffer)) | mark << buffer;
     }
     bf16x8* const to = (bf16x8*)(lds.v[buffer] + piece * kVStride + block * 32);
     to[0] = widened(y[0], y[2], scale);
     to[1] = widened(y[1], y[3], scale);
-    lds.nan[buffer][piece][block] = (uint16_t)where;
-    if ((tid & 63) == 0) {
-      lds.marks[buffer].nan[wave] = some;
-      lds.marks[buffer].there[block] = left > 0;
-    }
+  }
+  // Marks of both buffers as put_v expects to find them.
+  __device__ void clear_marks() const {
+    if (tid < (int)(sizeof(lds.marks) / 4)) ((uint32_t*)lds.marks)[tid] = 0;
+    for (int i = tid; i < (int)(sizeof(lds.nan) / 4); i += kThreads) ((uint32_t*)lds.nan)[i] = 0;
   }
 
   __device__ bf16x8 k_operand(int buffer, int kb, int ks) const {
@@ -114,6 +126,7 @@ struct RowsWalk {
   bf16x8 q[KS];
   f32x16 o[EB];
   float m, l;
+  int marked = 0;
   int limit, vis_wave, vis_first;      // keys that the lane's row sees; that the wave's last and first rows see
 
   __device__ __forceinline__ void scores(int buffer, f32x16 (&x)[2]) const {
@@ -130,15 +143,15 @@ struct RowsWalk {
   // what the buffer holds, for nobody).
   __device__ __forceinline__ void compute(int s, f32x16 (&x)[2], f32x16 (&y)[2]) {
     const u32x4 marks = *(const u32x4*)&lds.marks[s & 1];
-    const uint32_t mask = __builtin_amdgcn_readfirstlane(marks[0]), nan = __builtin_amdgcn_readfirstlane(marks[2] | marks[3]);
+    const uint32_t missing = __builtin_amdgcn_readfirstlane(marks[0]), nan = __builtin_amdgcn_readfirstlane(marks[2] | marks[3]);
     const bool cut = (s + 1) * kStep > vis_first;
-    if (cut || mask != 0x01010101) {
+    if (cut || missing) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int in = kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
-          if (s * kStep + in >= limit || !(mask >> (in / 16 * 8) & 1)) x[kb][i] = -INFINITY;
+          if (s * kStep + in >= limit || (missing >> (in / 16 * 8) & 1)) x[kb][i] = -INFINITY;
         }
     }
     float top = x[0][0];
@@ -172,11 +185,11 @@ struct RowsWalk {
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb) o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(s & 1, eb, j), p[j], o[eb], 0, 0, 0);
-    if (nan) {      // rows that see a NaN value are NaN in its column
+    if (__builtin_expect(nan != 0, 0)) {      // rows that see a NaN value are NaN in its column
       uint64_t seen = 0;
       for (int b = 0; b < 4; ++b) {
         const int n = limit - s * kStep - 16 * b;
-        if (mask >> (8 * b) & 1) seen |= (uint64_t)(n >= 16 ? 0xffff : n <= 0 ? 0 : (1 << n) - 1) << (16 * b);
+        if (!(missing >> (8 * b) & 1)) seen |= (uint64_t)(n >= 16 ? 0xffff : n <= 0 ? 0 : (1 << n) - 1) << (16 * b);
       }
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb)
@@ -208,40 +221,39 @@ struct RowsWalk {
     for (int eb = 0; eb < EB; ++eb) o[eb] = f32x16{};
     if (s0 < end) {
       const auto at_most = [&](int s) { return s < end ? s : end - 1; };
-      const auto counts = [&](int number, int step) { return cache_counts(step * 4 + block, vis, number, a.pages) ? vis - step * kStep - block * 16 : 0; };
-      const auto page_of = [&](int number) { return number >= 0 && number < a.pages ? number : 0; };
-      // numbers of the pages of the wave's block in this step and the next three
-      int n0 = find(row, s0, vis), n1 = find(row, at_most(s0 + 1), vis), n2 = find(row, at_most(s0 + 2), vis);
+      // the wave's block of this step, of the next and of the one behind it
+      Block b0 = found(number(row, s0, vis), s0, vis, head), b1 = found(number(row, at_most(s0 + 1), vis), at_most(s0 + 1), vis, head),
+            b2 = found(number(row, at_most(s0 + 2), vis), at_most(s0 + 2), vis, head);
       {
         Piece k0 = {}, k1 = {}, v0 = {};
         if (brings_k()) {
-          k0 = load(a.k_codes, a.k_scale, page_of(n0), s0, head);
-          k1 = load(a.k_codes, a.k_scale, page_of(n1), at_most(s0 + 1), head);
+          k0 = load(a.k_codes, a.k_scale, b0);
+          k1 = load(a.k_codes, a.k_scale, b1);
         }
-        if (brings_v()) v0 = load(a.v_codes, a.v_scale, page_of(n0), s0, head);
+        if (brings_v()) v0 = load(a.v_codes, a.v_scale, b0);
         __syncthreads();                            // the unit before has been read
         if (brings_k()) {
           put_k(k0, s0 & 1);
           put_k(k1, (s0 + 1) & 1);
         }
-        if (brings_v()) put_v(v0, s0 & 1, counts(n0, s0));
+        if (brings_v()) put_v(v0, s0 & 1, b0.left, marked);
       }
       __syncthreads();
       f32x16 x[2], y[2];
       scores(s0 & 1, x);
       __syncthreads();                              // (the first step's scores have been formed: its K makes room below)
-      int s = s0;
+      int s = s0, n3 = number(row, at_most(s0 + 3), vis);
       const auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2]) __attribute__((always_inline)) {
-        const int sk = at_most(s + 2), sv = at_most(s + 1);
         Piece kk = {}, vv = {};
-        if (brings_k()) kk = load(a.k_codes, a.k_scale, page_of(n2), sk, head);
-        if (brings_v()) vv = load(a.v_codes, a.v_scale, page_of(n1), sv, head);
-        const int left = counts(n1, sv);
-        n1 = n2;
-        n2 = find(row, at_most(s + 3), vis);
+        if (brings_k()) kk = load(a.k_codes, a.k_scale, b2);
+        if (brings_v()) vv = load(a.v_codes, a.v_scale, b1);
+        const int left = b1.left;
+        b1 = b2;
+        b2 = found(n3, at_most(s + 3), vis, head);
+        n3 = number(row, at_most(s + 4), vis);
         if (s * kStep < vis_wave) compute(s, now, next);
         if (brings_k()) put_k(kk, s & 1);
-        if (brings_v()) put_v(vv, (s + 1) & 1, left);
+        if (brings_v()) put_v(vv, (s + 1) & 1, left, marked);
         __syncthreads();
         return ++s < end;
       };
@@ -285,6 +297,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(CachePlan 
   CacheLeft left = {0, -1, 0, 0};
   if (share < workers) {
     RowsWalk<HS> walk(p.a, shared);
+    walk.clear_marks();                             // (a barrier stands before the first use)
     float* const slots = p.partial + share * 2 * CachePlan::slot(kCacheRowsTile, HS);
     shares.walk(p.a, kCacheRowsTile, shares.cut(all, share, workers), shares.cut(all, share + 1, workers),
                 [&](const CacheUnits<>& u, int seq, int head, int tile, int s0, int end, int of) __attribute__((always_inline)) {
