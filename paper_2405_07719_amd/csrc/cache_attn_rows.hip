@@ -139,6 +139,16 @@ struct RowsWalk {
     }
   }
 
+  // Operands of group n of a step's products: the scores of step s + 1, then the products with V of step s.
+  static constexpr int kGroups = KS + 2 * EB;
+  __device__ __forceinline__ void operands(int s, int n, bf16x8 (&f)[2]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      f[i] = n < KS ? k_operand((s + 1) & 1, i, n) : v_operand(s & 1, (n - KS) % (EB / 2) * 2 + i, (n - KS) / (EB / 2));
+  }
+  // How many of a step's 32 weights are formed before group n.
+  static constexpr int weights_before(int n) { return n <= KS ? 24 * n / KS : n - KS >= EB ? 32 : 24 + 8 * (n - KS) / EB; }
+
   // The vector work and products of step s, whose scores are x, and the scores of step s + 1 into y (behind the last step: of
   // what the buffer holds, for nobody).
   __device__ __forceinline__ void compute(int s, f32x16 (&x)[2], f32x16 (&y)[2]) {
@@ -154,6 +164,9 @@ struct RowsWalk {
           if (s * kStep + in >= limit || (missing >> (in / 16 * 8) & 1)) x[kb][i] = -INFINITY;
         }
     }
+    bf16x8 f[3][2];
+    operands(s, 0, f[0]);
+    operands(s, 1, f[1]);
     float top = x[0][0];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -169,22 +182,33 @@ struct RowsWalk {
       for (int eb = 0; eb < EB; ++eb) o[eb] *= alpha;
     }
     const float use = m == -INFINITY ? 0.0f : m;
-    scores((s + 1) & 1, y);
     bf16x8 p[4];
     float sum = 0.0f;
+    // Two products to a group, whose operands are on their way from LDS since two groups before; the groups are kept apart, or
+    // the compiler would read every operand just ahead of its product.
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int n = 0; n < kGroups; ++n) {
+      if (n + 2 < kGroups) operands(s, n + 2, f[(n + 2) % 3]);
+      if (n < KS) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float w = __builtin_amdgcn_exp2f(x[kb][i] * a.scale_log2e - use);
-        sum += w;
-        p[kb * 2 + i / 8][i % 8] = (__bf16)w;
+        for (int kb = 0; kb < 2; ++kb)
+          y[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % 3][kb], q[n], n ? y[kb] : f32x16{}, 0, 0, 0);
+      } else {
+        const int j = (n - KS) / (EB / 2), eb = (n - KS) % (EB / 2) * 2;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) o[eb + i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % 3][i], p[j], o[eb + i], 0, 0, 0);
       }
+      // 24 exponentials beside the products of the scores, the last 8 beside the first products with V
+#pragma unroll
+      for (int i = weights_before(n); i < weights_before(n + 1); ++i) {
+        const float w = __builtin_amdgcn_exp2f(x[i / 16][i % 16] * a.scale_log2e - use);
+        sum += w;
+        p[i / 8][i % 8] = (__bf16)w;
+      }
+      asm volatile("" : "+v"(sum));      // (or the additions would sink to the end, all weights waiting for them in registers)
+      __builtin_amdgcn_sched_barrier(0);
+    }
     l += sum;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int eb = 0; eb < EB; ++eb) o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(s & 1, eb, j), p[j], o[eb], 0, 0, 0);
     if (__builtin_expect(nan != 0, 0)) {      // rows that see a NaN value are NaN in its column
       uint64_t seen = 0;
       for (int b = 0; b < 4; ++b) {
