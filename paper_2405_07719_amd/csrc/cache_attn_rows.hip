@@ -57,10 +57,11 @@ struct RowsWalk {
   // The wave's block of a step: where its page's scales and its own codes are, of K as of V, and how many of its tokens count.
   // (A page that is not there reads page 0, unconditionally: a load under a condition would be waited for where it stands.)
   struct Block { int64_t place, codes; int left; };
-  __device__ int number(const int32_t* row, int step, int vis) const {
-    return __builtin_amdgcn_readfirstlane(row[cache_entry(step * 4 + block, vis, a.page_shift)]);
-  }
-  __device__ Block found(int number, int step, int vis, int head) const {
+  // (The number stays in a vector register until it is looked at, a step later: what is asked for before it would have to arrive
+  // first.)
+  __device__ int number(const int32_t* row, int step, int vis) const { return row[cache_entry(step * 4 + block, vis, a.page_shift)]; }
+  __device__ Block found(int looked_up, int step, int vis, int head) const {
+    const int number = __builtin_amdgcn_readfirstlane(looked_up);
     const bool counts = cache_counts(step * 4 + block, vis, number, a.pages);
     const int inside = (step * kStep + block * 16) & ((1 << a.page_shift) - 1);
     const int64_t place = (int64_t)(counts ? number : 0) * a.hk + head;
