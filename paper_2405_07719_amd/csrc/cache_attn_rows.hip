@@ -10,9 +10,10 @@
 // leaves: of 16 tokens of V the lanes below 32 need 0-3 and 8-11, the others 4-7 and 12-15, which is the order in which they
 // are written to LDS.
 //
-// Step s: the maxima of its scores; then, side by side, the scores of step s + 1 (matrix cores), the exponentials of step s
-// (vector ALU) and the products with V; while the codes of K two steps ahead and of V one step ahead are on their way.
-// K and V have two buffers each, and a step ends with the one barrier that they need.
+// Step s puts the codes of K two steps ahead and of V one step ahead, which came during the step before, into LDS and asks for
+// those behind them; then, side by side, the scores of step s + 1 and the products with V of step s (matrix cores), the
+// exponentials of step s and the maxima of step s + 1 (vector ALU).  K and V have two buffers each, and a step ends with the one
+// barrier that they need.
 #include "cache_attn_device.h"
 
 namespace usp {
@@ -151,29 +152,26 @@ struct RowsWalk {
   static constexpr int weights_before(int n) { return n <= KS ? 24 * n / KS : n - KS >= EB ? 32 : 24 + 8 * (n - KS) / EB; }
 
   // The vector work and products of step s, whose scores are x, and the scores of step s + 1 into y (behind the last step: of
-  // what the buffer holds, for nobody).
-  __device__ __forceinline__ void compute(int s, f32x16 (&x)[2], f32x16 (&y)[2]) {
-    const u32x4 marks = *(const u32x4*)&lds.marks[s & 1];
+  // what the buffer holds, for nobody).  top: the largest of the lane's scores, then of the next step's, none of them masked.
+  __device__ __forceinline__ void compute(int s, u32x4 marks, f32x16 (&x)[2], f32x16 (&y)[2], float& top) {
     const uint32_t missing = __builtin_amdgcn_readfirstlane(marks[0]), nan = __builtin_amdgcn_readfirstlane(marks[2] | marks[3]);
     const bool cut = (s + 1) * kStep > vis_first;
     if (cut || missing) {
+      top = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int in = kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
           if (s * kStep + in >= limit || (missing >> (in / 16 * 8) & 1)) x[kb][i] = -INFINITY;
+          top = fmaxf(top, x[kb][i]);
         }
     }
     bf16x8 f[3][2];
     operands(s, 0, f[0]);
     operands(s, 1, f[1]);
-    float top = x[0][0];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
-    top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2e;
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_int(top), __float_as_int(top), false, false);
+    top = fmaxf(__int_as_float(both[0]), __int_as_float(both[1])) * a.scale_log2e;
     // The value that is subtracted need not be the maximum: it moves where a row's grows by more than 2^8.
     if (__ballot(top > m + 8.0f)) {
       const float now = fmaxf(m, top), use = now == -INFINITY ? 0.0f : now, alpha = exp2f(m - use);
@@ -186,7 +184,8 @@ struct RowsWalk {
     bf16x8 p[4];
     float sum = 0.0f;
     // Two products to a group, whose operands are on their way from LDS since two groups before; the groups are kept apart, or
-    // the compiler would read every operand just ahead of its product.
+    // the compiler would read every operand just ahead of its product.  24 of the exponentials stand beside the scores, the last
+    // 8 and the next step's maxima beside the products with V.
 #pragma unroll
     for (int n = 0; n < kGroups; ++n) {
       if (n + 2 < kGroups) operands(s, n + 2, f[(n + 2) % 3]);
@@ -199,7 +198,6 @@ struct RowsWalk {
 #pragma unroll
         for (int i = 0; i < 2; ++i) o[eb + i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % 3][i], p[j], o[eb + i], 0, 0, 0);
       }
-      // 24 exponentials beside the products of the scores, the last 8 beside the first products with V
 #pragma unroll
       for (int i = weights_before(n); i < weights_before(n + 1); ++i) {
         const float w = __builtin_amdgcn_exp2f(x[i / 16][i % 16] * a.scale_log2e - use);
@@ -207,6 +205,13 @@ struct RowsWalk {
         p[i / 8][i % 8] = (__bf16)w;
       }
       asm volatile("" : "+v"(sum));      // (or the additions would sink to the end, all weights waiting for them in registers)
+      if (n == KS + EB) top = y[0][0];
+      if (n >= KS + EB) {
+        constexpr int kEach = 32 / EB;
+#pragma unroll
+        for (int i = (n - KS - EB) * kEach; i < (n - KS - EB + 1) * kEach; ++i) top = fmaxf(top, y[i / 16][i % 16]);
+        asm volatile("" : "+v"(top));
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
     l += sum;
@@ -246,16 +251,23 @@ struct RowsWalk {
     for (int eb = 0; eb < EB; ++eb) o[eb] = f32x16{};
     if (s0 < end) {
       const auto at_most = [&](int s) { return s < end ? s : end - 1; };
-      // the wave's block of this step, of the next and of the one behind it
-      Block b0 = found(number(row, s0, vis), s0, vis, head), b1 = found(number(row, at_most(s0 + 1), vis), at_most(s0 + 1), vis, head),
-            b2 = found(number(row, at_most(s0 + 2), vis), at_most(s0 + 2), vis, head);
+      const auto block_of = [&](int s) { return found(number(row, at_most(s), vis), at_most(s), vis, head); };
+      const Block b0 = block_of(s0), b1 = block_of(s0 + 1);
+      Block bk = block_of(s0 + 3), bv = block_of(s0 + 2);      // of the codes that are asked for next
+      int ahead = number(row, at_most(s0 + 4), vis), left;     // left: tokens of the V block that is on its way
+      Piece kk = {}, vv = {};
       {
         Piece k0 = {}, k1 = {}, v0 = {};
         if (brings_k()) {
           k0 = load(a.k_codes, a.k_scale, b0);
           k1 = load(a.k_codes, a.k_scale, b1);
+          kk = load(a.k_codes, a.k_scale, bv);
         }
-        if (brings_v()) v0 = load(a.v_codes, a.v_scale, b0);
+        if (brings_v()) {
+          v0 = load(a.v_codes, a.v_scale, b0);
+          vv = load(a.v_codes, a.v_scale, b1);
+        }
+        left = b1.left;
         __syncthreads();                            // the unit before has been read
         if (brings_k()) {
           put_k(k0, s0 & 1);
@@ -267,18 +279,23 @@ struct RowsWalk {
       f32x16 x[2], y[2];
       scores(s0 & 1, x);
       __syncthreads();                              // (the first step's scores have been formed: its K makes room below)
-      int s = s0, n3 = number(row, at_most(s0 + 3), vis);
+      float top = x[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+      int s = s0;
       const auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2]) __attribute__((always_inline)) {
-        Piece kk = {}, vv = {};
-        if (brings_k()) kk = load(a.k_codes, a.k_scale, b2);
-        if (brings_v()) vv = load(a.v_codes, a.v_scale, b1);
-        const int left = b1.left;
-        b1 = b2;
-        b2 = found(n3, at_most(s + 3), vis, head);
-        n3 = number(row, at_most(s + 4), vis);
-        if (s * kStep < vis_wave) compute(s, now, next);
-        if (brings_k()) put_k(kk, s & 1);
+        const u32x4 marks = *(const u32x4*)&lds.marks[s & 1];
+        if (brings_k()) put_k(kk, s & 1);           // of step s + 2
         if (brings_v()) put_v(vv, (s + 1) & 1, left, marked);
+        if (brings_k()) kk = load(a.k_codes, a.k_scale, bk);
+        if (brings_v()) vv = load(a.v_codes, a.v_scale, bv);
+        left = bv.left;
+        bv = bk;
+        bk = found(ahead, at_most(s + 4), vis, head);
+        ahead = number(row, at_most(s + 5), vis);
+        if (s * kStep < vis_wave) compute(s, marks, now, next, top);
         __syncthreads();
         return ++s < end;
       };
