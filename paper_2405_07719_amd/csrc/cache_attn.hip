@@ -236,10 +236,10 @@ struct Sum {
     l = l * keep + l2 * take;
     o = o * keep + o2 * take;
   }
-  // row `row` (of a tile's) of a unit, columns e .. e + 3
-  template <int HS, typename Units>
-  __device__ void write(const CacheAttnArgs& a, const Units& u, int head, int64_t row, int e) const {
-    const int in = (int)(row / a.group), hq = head * a.group + (int)(row - (int64_t)in * a.group), token = u.cu + in;
+  // row `row` of a unit's request and KV head, columns e .. e + 3
+  template <int HS>
+  __device__ void write(const CacheAttnArgs& a, const CacheLeft& unit, int64_t row, int e) const {
+    const int in = (int)(row / a.group), hq = unit.head * a.group + (int)(row - (int64_t)in * a.group), token = unit.cu + in;
     const f32x4 y = o * (l == 0.0f ? 0.0f : 1.0f / l);
     const int64_t to = ((int64_t)token * (a.hk * a.group) + hq) * HS + e;
     if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to) = __builtin_convertvector(y, bf16x4);
@@ -272,8 +272,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
   const I n = stop - pos, mine = pos + n / kWaves * wave + (n % kWaves * wave + kWaves - 1) / kWaves,
           next = pos + n / kWaves * (wave + 1) + (n % kWaves * (wave + 1) + kWaves - 1) / kWaves;
   Walk<HS> walk(p, threadIdx.x & 63);
-  int first = 0;
-  CacheLeft end = {0, -1, 0, 0};
+  int first = 0, end_rows = 0, end_head = 0, end_tile = 0, end_cu = 0;
   shares.walk(p.a, kTile, mine, next, [&](const CacheUnits<I>& u, int seq, int head, int tile, int s0, int s1, int of) __attribute__((always_inline)) {
     const bool begins = s0 == 0, ends = s1 == of;
     walk.unit(u, seq, head, tile, s0, s1);
@@ -281,26 +280,26 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
       walk.write();
     } else {
       walk.put(lds.slot[2 * wave + begins]);
-      if (begins) end = CacheLeft{0, seq, head, tile};
+      if (begins) end_rows = walk.rows, end_head = head, end_tile = tile, end_cu = u.cu;
       else first = ends ? 2 : 1;
     }
   });
   // A wave without steps lets the unit that goes on around it pass (it has no partial result: 3).
   if ((threadIdx.x & 63) == 0) {
     lds.first[wave] = mine < next ? first : 3;
-    lds.end[wave] = end;
+    lds.end[wave] = CacheLeft{0, end_rows, end_head, end_tile, end_cu};
   }
   __syncthreads();
   // Units that waves share, each from the wave that has its beginning, or from the first wave, where the unit began in a workgroup
   // before.
   constexpr int kTeam = HS / 4;
   const int row = threadIdx.x / kTeam, e = threadIdx.x % kTeam * 4;
-  CacheLeft left = {0, -1, 0, 0};
+  int left_first = 0, left_end = -1;      // what the workgroup leaves: the second as the wave that has it
   float* const slots = p.partial + share * 2 * CachePlan::slot(kTile, HS);
   for (int w = 0; w < kWaves; ++w) {
     const int f = lds.first[w];
     for (int begins = w ? 1 : 0; begins < 2; ++begins) {
-      if (begins ? lds.end[w].seq < 0 : f != 1 && f != 2) continue;
+      if (begins ? lds.end[w].rows == 0 : f != 1 && f != 2) continue;
       bool ended = !begins && f == 2;
       Sum sum = {-INFINITY, 0.0f, {0, 0, 0, 0}};
       for (int x = w; ; ++x) {
@@ -316,68 +315,89 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
         else sum.add(ml[0], ml[1], o);
       }
       if (begins && ended) {
-        const CacheUnits<I> u = shares.units(p.a, lds.end[w].seq, kTile);
-        if (row < u.rows(p.a, lds.end[w].tile, kTile)) sum.template write<HS>(p.a, u, lds.end[w].head, (int64_t)lds.end[w].tile * kTile + row, e);
+        const CacheLeft& unit = lds.end[w];
+        if (row < unit.rows) sum.template write<HS>(p.a, unit, (int64_t)unit.tile * kTile + row, e);
       } else {
         float* const to = slots + (begins ? CachePlan::slot(kTile, HS) : 0);
         if (row < kTile) {
           if (e == 0) ((f32x2*)to)[row] = f32x2{sum.m, sum.l};
           *(f32x4*)(to + 2 * kTile + row * HS + e) = sum.o;
         }
-        if (begins) left.seq = lds.end[w].seq, left.head = lds.end[w].head, left.tile = lds.end[w].tile;
-        else left.first = ended ? 2 : 1;
+        if (begins) left_end = w;
+        else left_first = ended ? 2 : 1;
       }
     }
   }
-  if (!p.whole && threadIdx.x == 0) p.left[share] = left;
+  if (!p.whole && threadIdx.x == 0) {
+    const CacheLeft& end = lds.end[left_end < 0 ? 0 : left_end];
+    p.left[share] = CacheLeft{left_first, left_end < 0 ? 0 : end.rows, end.head, end.tile, end.cu};
+  }
 }
 
-// Joins the partial results of one unit: the beginning that worker w left, then what the workers behind it left up to the unit's
-// end.  A team of HS / 4 threads adds up a row, four columns to a thread; the teams of a workgroup share the parts of one
-// row where there are many, else they have a row each.  blockIdx.y: which of the unit's rows.
+// Joins the partial results of units that workgroups share: of each the beginning that worker w left, then what the workers behind
+// it left up to the unit's end.  A team of HS / 4 threads adds up parts of a row, four columns to a thread, in the order of the
+// keys; several teams have a row between them, the more the fewer rows there are, so that a few long units are joined by the
+// whole chip too.
 template <int HS>
 __global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan p, int rows_per_tile) {
-  constexpr int kTeam = HS / 4, kTeams = kJoinThreads / kTeam;
+  constexpr int kTeam = HS / 4, kTeams = kJoinThreads / kTeam, kWorkers = kPlanCUs;
+  static_assert(kWorkers == kJoinThreads, "a thread to each worker");
   __shared__ f32x4 sums[kTeams][kTeam];
   __shared__ f32x2 mls[kTeams];
-  const int64_t slot = CachePlan::slot(rows_per_tile, HS);
+  __shared__ CacheLeft left[kWorkers];
+  __shared__ int leaders[kWorkers], counts[kJoinThreads / 64];
   const CacheAttnArgs& a = p.a;
-  const int w = blockIdx.x, lane = threadIdx.x & 63, team = threadIdx.x / kTeam, e = threadIdx.x % kTeam * 4;
-  const CacheLeft mine = p.left[w];
-  if (mine.seq < 0) return;
-  int parts = 1;                                     // parts 1 .. parts - 1 are those of workers w + 1 ...
-  for (;;) {
-    const int x = w + parts + lane;
-    const uint64_t on = __ballot(x < p.workers && p.left[x < p.workers ? x : w].first == 1);
-    if (on != ~0ull) {
-      parts += __builtin_ctzll(~on);
-      break;
-    }
-    parts += 64;
+  const int64_t slot = CachePlan::slot(rows_per_tile, HS);
+  const int tid = threadIdx.x, lane = tid & 63, team = tid / kTeam, e = tid % kTeam * 4;
+  left[tid] = p.left[tid];
+  const uint64_t mine = __ballot(left[tid].rows > 0);
+  if (lane == 0) counts[tid >> 6] = __builtin_popcountll(mine);
+  __syncthreads();
+  int units = 0, at = __builtin_popcountll(mine & ((1ull << lane) - 1));
+  for (int w = 0; w < kJoinThreads / 64; ++w) {
+    if (w < tid >> 6) at += counts[w];
+    units += counts[w];
   }
-  parts += w + parts < p.workers;                    // the one in which it ends
-  const CacheUnits<> u(a, mine.seq, rows_per_tile);
-  const int rows = u.rows(a, mine.tile, rows_per_tile);
-  const bool shared = parts >= kTeams;               // many parts to a row
-  const auto slot_of = [&](int x) { return p.partial + (x ? 2 * (int64_t)(w + x) : 2 * (int64_t)w + 1) * slot; };
-  const int step = shared ? gridDim.y : gridDim.y * kTeams;
-  for (int row = shared ? blockIdx.y : blockIdx.y * kTeams + team; row < rows; row += step) {
+  if (left[tid].rows > 0) leaders[at] = tid;
+  __syncthreads();
+  int together = 1;                                  // rows that a workgroup has at a time
+  while (together < kTeams && units * rows_per_tile > together * (int)gridDim.x) together *= 2;
+  const int share = kTeams / together, items = rows_per_tile / together;
+  for (int item = blockIdx.x; item < units * items; item += gridDim.x) {
+    const int w = leaders[item / items], first_row = item % items * together;
+    const CacheLeft unit = left[w];
+    if (first_row >= unit.rows) continue;
+    int parts = 1;                                   // parts 1 .. parts - 1 are those of workers w + 1 ...
+    for (;;) {
+      const int x = w + parts + lane;
+      const uint64_t on = __ballot(x < kWorkers && left[x & (kWorkers - 1)].first == 1);
+      if (on != ~0ull) {
+        parts += __builtin_ctzll(~on);
+        break;
+      }
+      parts += 64;
+    }
+    parts += w + parts < kWorkers;                   // the one in which it ends
+    const int row = first_row + team / share, from = team % share;
+    const bool real = row < unit.rows;
+    // (teams behind one another have parts behind one another)
+    const int begin = parts * from / share, stop = real ? parts * (from + 1) / share : begin;
     Sum sum = {-INFINITY, 0.0f, {0, 0, 0, 0}};
 #pragma unroll 4
-    for (int x = shared ? team : 0; x < parts; x += shared ? kTeams : 1) {
-      const float* const at = slot_of(x);
-      const f32x2 ml = ((const f32x2*)at)[row];
-      sum.add(ml[0], ml[1], *(const f32x4*)(at + 2 * rows_per_tile + row * HS + e));
+    for (int x = begin; x < stop; ++x) {
+      const float* const part = p.partial + (x ? 2 * (int64_t)(w + x) : 2 * (int64_t)w + 1) * slot;
+      const f32x2 ml = ((const f32x2*)part)[row];
+      sum.add(ml[0], ml[1], *(const f32x4*)(part + 2 * rows_per_tile + row * HS + e));
     }
-    if (shared) {                                    // the teams' sums, in their order
-      __syncthreads();
-      sums[team][threadIdx.x % kTeam] = sum.o;
+    if (share > 1) {
+      __syncthreads();                               // (the item before has been read)
+      sums[team][tid % kTeam] = sum.o;
       if (e == 0) mls[team] = f32x2{sum.m, sum.l};
       __syncthreads();
-      if (team) continue;
-      for (int t = 1; t < kTeams; ++t) sum.add(mls[t][0], mls[t][1], sums[t][threadIdx.x]);
+      if (from == 0)
+        for (int t = team + 1; t < team + share; ++t) sum.add(mls[t][0], mls[t][1], sums[t][tid % kTeam]);
     }
-    sum.template write<HS>(a, u, mine.head, (int64_t)mine.tile * rows_per_tile + row, e);
+    if (real && from == 0) sum.template write<HS>(a, unit, (int64_t)unit.tile * rows_per_tile + row, e);
   }
 }
 
@@ -417,7 +437,7 @@ int launch_cache_attn(const CacheAttnArgs& a, int max_q, hipStream_t stream) {
   const int st = !few ? launch_cache_attn_rows(p, stream) : a.hs == 128 ? launch_few<128>(p, stream) : launch_few<64>(p, stream);
   if (st != USP_OK) return st;
   if (!p.whole) {
-    const dim3 grid(p.workers, few ? 4 : 16);
+    const dim3 grid(kPlanCUs * 4);
     if (a.hs == 128) cache_attn_join_kernel<128><<<grid, kJoinThreads, 0, stream>>>(p, rows_of(few));
     else cache_attn_join_kernel<64><<<grid, kJoinThreads, 0, stream>>>(p, rows_of(few));
   }

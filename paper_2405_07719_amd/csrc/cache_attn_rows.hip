@@ -19,7 +19,7 @@
 namespace usp {
 namespace {
 
-constexpr int kThreads = 512, kStep = kCacheStep, kRows = 32;
+constexpr int kThreads = 512, kStep = kCacheStep, kRows = 32, kLeastSteps = 4;
 
 template <int HS> constexpr int k_stride() { return HS * 2 + 16; }
 constexpr int kVStride = kStep * 2 + 16;
@@ -335,8 +335,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(CachePlan 
   const int64_t all = shared.shares.count(p.a, kCacheRowsTile);
   // The workgroups of an XCD (blockIdx % 8) have shares that follow on one another: mostly of one KV head.
   const int n = (int)gridDim.x, share = n % 8 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (n / 8) + (int)blockIdx.x / 8;
-  const int workers = all < n ? (int)all : n;
-  CacheLeft left = {0, -1, 0, 0};
+  // (a share of fewer steps would cost less than the partial results that it leaves: 256 rows are the bytes of eight steps)
+  const int64_t most = (all + kLeastSteps - 1) / kLeastSteps;
+  const int workers = most < n ? (int)most : n;
+  int first = 0, end_rows = 0, end_head = 0, end_tile = 0, end_cu = 0;      // as in CacheLeft
   if (share < workers) {
     RowsWalk<HS> walk(p.a, shared);
     walk.clear_marks();                             // (a barrier stands before the first use)
@@ -345,11 +347,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_rows_kernel(CachePlan 
                 [&](const CacheUnits<>& u, int seq, int head, int tile, int s0, int end, int of) __attribute__((always_inline)) {
                   const bool begins = s0 == 0, ends = end == of;
                   walk.unit(u, seq, head, tile, s0, end, begins && ends, slots + (begins ? CachePlan::slot(kCacheRowsTile, HS) : 0));
-                  if (!begins) left.first = ends ? 2 : 1;
-                  else if (!ends) left.seq = seq, left.head = head, left.tile = tile;
+                  if (!begins) first = ends ? 2 : 1;
+                  else if (!ends) end_rows = u.rows(p.a, tile, kCacheRowsTile), end_head = head, end_tile = tile, end_cu = u.cu;
                 });
   }
-  if (threadIdx.x == 0) p.left[share] = left;
+  if (threadIdx.x == 0) p.left[share] = CacheLeft{first, end_rows, end_head, end_tile, end_cu};
 }
 
 template <int HS>

@@ -131,8 +131,9 @@ __host__ __device__ inline bool cache_counts(int b, int vis, int number, int64_t
 }
 
 // What a worker (a wave, or a workgroup) leaves for the joining launch: `first`: 0, or its share begins inside a unit, which goes
-// on behind it (1) or ends in it (2); seq >= 0: its share ends inside the unit (seq, head, tile), which begins in it.
-struct CacheLeft { int first, seq, head, tile; };
+// on behind it (1) or ends in it (2); rows > 0: its share ends inside a unit of so many rows, which begins in it: (KV head, tile) of
+// the request whose first row is cu.
+struct CacheLeft { int first, rows, head, tile, cu; };
 
 struct CachePlan {
   CacheAttnArgs a;
