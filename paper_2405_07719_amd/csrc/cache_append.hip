@@ -69,7 +69,8 @@ template <> struct Two<float> {
 
 // One page and head of K (V_TILES false) or V.  x: the head's elements in the row of the first token; `n` tokens from place
 // `old` on; codes: the page's codes of the head.
-template <typename T, int HS, bool V_TILES>
+// PAST_CACHES: values are read nontemporally.
+template <typename T, int HS, bool V_TILES, bool PAST_CACHES>
 struct Page {
   // K: eight elements of a row to a lane; V: two columns to a lane, of 16 tokens (hs 128) or 8 (hs 64)
   static constexpr int kPer = V_TILES ? 2 : 8, kPairs = kPer / 2, kLanesPerRow = HS / kPer, kGroups = 64 / kLanesPerRow,
@@ -90,7 +91,7 @@ struct Page {
   __device__ int column() const { return lane % kLanesPerRow * kPer; }
 
   // A lane's elements of a tile.  Places that are not given read one that is: a load under a condition would be waited for
-  // where it stands, one after the other.  Nontemporal: read once (38 thousand rows 66 us, so 61).
+  // where it stands, one after the other.
   __device__ void load(int tile, Raw (&v)[kTokens][kPairs]) const {
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
@@ -98,10 +99,11 @@ struct Page {
       p = p < 0 ? 0 : p < n ? p : n - 1;
       const T* const from = x + p * stride + column();
       if constexpr (V_TILES) {
-        v[i][0] = __builtin_nontemporal_load((const Raw*)from);
+        v[i][0] = PAST_CACHES ? __builtin_nontemporal_load((const Raw*)from) : *(const Raw*)from;
       } else {
 #pragma unroll
-        for (int w = 0; w < (int)sizeof(T) / 2; ++w) ((u32x4*)v[i])[w] = __builtin_nontemporal_load((const u32x4*)from + w);
+        for (int w = 0; w < (int)sizeof(T) / 2; ++w)
+          ((u32x4*)v[i])[w] = PAST_CACHES ? __builtin_nontemporal_load((const u32x4*)from + w) : ((const u32x4*)from)[w];
       }
     }
   }
@@ -249,7 +251,7 @@ struct Page {
   }
 };
 
-template <typename T, int HS>
+template <typename T, int HS, bool PAST_CACHES>
 __global__ __launch_bounds__(kThreads) void cache_append_kernel(CacheAppendArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
@@ -285,8 +287,8 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(CacheAppendArgs 
       if (again) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // the stretch before wrote to this page
       const T* const x = (const T*)a.x[tensor] + row * a.stride[tensor] + head * HS;
       uint8_t* const codes = a.codes[tensor] + place * page * HS;
-      if (tensor) Page<T, HS, true>{x, a.stride[1], codes, lane, old, n}.write(a.scale[1] + place);
-      else Page<T, HS, false>{x, a.stride[0], codes, lane, old, n}.write(a.scale[0] + place);
+      if (tensor) Page<T, HS, true, PAST_CACHES>{x, a.stride[1], codes, lane, old, n}.write(a.scale[1] + place);
+      else Page<T, HS, false, PAST_CACHES>{x, a.stride[0], codes, lane, old, n}.write(a.scale[0] + place);
       row += n;
       if (row >= a.rows) break;
       slot = a.slots[row];
@@ -295,24 +297,31 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(CacheAppendArgs 
   }
 }
 
+template <typename T>
+void launch(const CacheAppendArgs& a, unsigned grid, bool past_caches, hipStream_t stream) {
+  const auto go = [&](auto kernel) { kernel<<<dim3(grid), kThreads, 0, stream>>>(a); };
+  if (a.hs == 128) past_caches ? go(cache_append_kernel<T, 128, true>) : go(cache_append_kernel<T, 128, false>);
+  else past_caches ? go(cache_append_kernel<T, 64, true>) : go(cache_append_kernel<T, 64, false>);
+}
+
 }  // namespace
 
 int launch_cache_append(const CacheAppendArgs& args, int dtype, hipStream_t stream) {
   CacheAppendArgs a = args;
-  // Rows in which a wave looks for pages that begin there.
-  a.window = a.rows <= 2048 ? 1 : a.rows <= USP_CACHE_MAX_REQUESTS ? 8 : 64;
+  // Rows in which a wave looks for pages that begin there.  More rows than there can be requests are stretches of several
+  // tokens: 38 thousand rows of 12 prompts take 67 us with 64 rows to a wave, 75 with 32 and 218 with 8, most of whose waves find
+  // nothing.  One token of each request is a page to a row: then a wave would have to write one page after the other.
+  const bool many = a.rows > USP_CACHE_MAX_REQUESTS;
+  a.window = many ? 64 : a.rows > 2048 ? 8 : 1;
   // (several launches where one would have 2^32 threads or more)
   const int64_t windows = (a.rows + a.window - 1) / a.window, most = max_workgroups(kThreads) * (kThreads / 64) / (2 * a.hk);
   for (a.first_window = 0; a.first_window < windows; a.first_window += most) {
-    const int64_t w = a.windows = windows - a.first_window < most ? windows - a.first_window : most;
-    const dim3 g((unsigned)((w * a.hk * 2 + kThreads / 64 - 1) / (kThreads / 64)));
-    if (dtype == USP_BF16) {
-      if (a.hs == 128) cache_append_kernel<__bf16, 128><<<g, kThreads, 0, stream>>>(a);
-      else cache_append_kernel<__bf16, 64><<<g, kThreads, 0, stream>>>(a);
-    } else {
-      if (a.hs == 128) cache_append_kernel<float, 128><<<g, kThreads, 0, stream>>>(a);
-      else cache_append_kernel<float, 64><<<g, kThreads, 0, stream>>>(a);
-    }
+    a.windows = windows - a.first_window < most ? windows - a.first_window : most;
+    const unsigned grid = (unsigned)((a.windows * a.hk * 2 + kThreads / 64 - 1) / (kThreads / 64));
+    // A long prompt's rows, read once, go past the caches (66 -> 61 us for the same rows); a few are in them still (64 rows: 6.4
+    // us, past the caches 6.9).
+    if (dtype == USP_BF16) launch<__bf16>(a, grid, many, stream);
+    else launch<float>(a, grid, many, stream);
   }
   return launch_status();
 }
