@@ -401,9 +401,14 @@ __global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan
   }
 }
 
-// Up to 16 rows of a request fit one product of the kernel that gives each wave units of its own; more go to the kernel for many
-// rows.  Both have one workgroup of eight waves to a CU.
-bool few_rows(int group, int max_q) { return (int64_t)group * (max_q < 1 ? 1 : max_q) <= 16; }
+// Requests of few rows go to the kernel that gives each wave units of its own, which reads the cache again for every 16 rows; the
+// one for many rows has a request's rows up to 256 at once, but a step of it takes as long for one as for all.  Measured with 8
+// KV heads of 128, here / there: 64 requests of 256 to 32768 tokens, 16 rows 169 us, 32 rows 295 / 393, 64 rows 547 / 404; 64
+// of 100 to 4000 tokens, 32 rows 63 / 134, 64 rows 94 / 141; one of 32768 tokens, 32 rows 28 / 38, 64 rows 38 / 40.  So 32 rows, and
+// 64 where the table has room for 8192 tokens at most.
+bool few_rows(int group, int max_q, int64_t most_tokens) {
+  return (int64_t)group * (max_q < 1 ? 1 : max_q) <= (most_tokens <= 8192 ? 64 : 32);
+}
 int rows_of(bool few) { return few ? kTile : kCacheRowsTile; }
 
 template <int HS, typename I>
@@ -424,16 +429,18 @@ int launch_few(const CachePlan& p, hipStream_t stream) {
 }  // namespace
 
 size_t cache_attn_workspace(int group, int hs, int max_q) {
-  return kPlanCUs * (sizeof(CacheLeft) + 2 * CachePlan::slot(rows_of(few_rows(group, max_q)), hs) * sizeof(float));
+  const bool few = few_rows(group, max_q, INT64_MAX);
+  return kPlanCUs * (sizeof(CacheLeft) + 2 * CachePlan::slot(rows_of(few), hs) * sizeof(float));
 }
 
 int launch_cache_attn(const CacheAttnArgs& a, int max_q, hipStream_t stream) {
-  const bool few = few_rows(a.group, max_q);
+  const int64_t most_tokens = (int64_t)a.max_pages << a.page_shift;
+  const bool few = few_rows(a.group, max_q, most_tokens);
   CachePlan p = {a, kPlanCUs, (CacheLeft*)a.workspace, nullptr, 0};
   p.partial = (float*)(p.left + p.workers);
   // Rows of the table that hold 4096 tokens at most, and a unit and more for every CU: a wave has eight steps of a unit at most, and
   // the joining launch would cost more than cutting units between workgroups gains.
-  p.whole = few && (int64_t)a.max_pages << a.page_shift <= 4096 && (int64_t)a.n_seqs * a.hk >= kPlanCUs;
+  p.whole = few && most_tokens <= 4096 && (int64_t)a.n_seqs * a.hk >= kPlanCUs;
   const int st = !few ? launch_cache_attn_rows(p, stream) : a.hs == 128 ? launch_few<128>(p, stream) : launch_few<64>(p, stream);
   if (st != USP_OK) return st;
   if (!p.whole) {

@@ -96,8 +96,11 @@ def test_ragged_rows(usp, hs, page, hq, hk, causal, most):
 @pytest.mark.parametrize("hs", [64, 128])
 @pytest.mark.parametrize("news", [[4], [8], [5, 2, 8], [16, 1]])
 def test_a_few_rows(usp, hs, news):
-    """Tiles of 16 and of 32 rows, full and not."""
-    Case(usp, sum(news) + hs, [300 + 200 * i for i in range(len(news))], news, 8, 2, hs, 32).check()
+    """One to four tiles of 16 rows and more, full and not; tables of up to 8192 tokens and beyond."""
+    case = Case(usp, sum(news) + hs, [300 + 200 * i for i in range(len(news))], news, 8, 2, hs, 32)
+    case.check()
+    case.table = np.concatenate([case.table, np.full((len(news), 8192 // 32), 0x7fffff03, dtype=np.int32)], 1)
+    case.check()
 
 
 @pytest.mark.parametrize("hs", [64, 128])

@@ -130,7 +130,7 @@ def test_cache_refusals(lib):
 def test_attention_workspace_depends_on_the_rows_of_a_tile_alone(lib):
     sizes = {(hs, hq, mq): usp.usp_cache_attn_workspace_bytes(cache(hs=hs), hq, mq) for hs in (64, 128) for hq in (2, 8, 64) for mq in (0, 1, 4, 5, 9, 4096)}
     assert max(sizes.values()) <= 96 << 20
-    assert sizes[128, 8, 1] == sizes[128, 8, 0] == sizes[128, 8, 4] == usp.usp_cache_attn_workspace_bytes(cache(pages=1000, page=128, hk=4), 16, 4)
+    assert sizes[128, 8, 1] == sizes[128, 8, 0] == sizes[128, 8, 4] == usp.usp_cache_attn_workspace_bytes(cache(pages=1000, page=128, hk=4), 16, 8)
 
 
 PLAN = """
