@@ -14,6 +14,10 @@
 // those behind them; then, side by side, the scores of step s + 1 and the products with V of step s (matrix cores), the
 // exponentials of step s and the maxima of step s + 1 (vector ALU).  K and V have two buffers each, and a step ends with the one
 // barrier that they need.
+//
+// Measured: 4096 rows of 32 heads over 49152 tokens (3.16 TFLOP) 2.8 ms, 1.11 to 1.15 PFLOP/s, matrix cores busy 55 % of the
+// cycles; a library product of 8192 x 8192 matrices reaches 1.11, of 16384 1.37.  Without the exponentials, or without bringing
+// codes to LDS, a step takes 8 to 9 % less: what is left is the two waves of a SIMD waiting for LDS operands and for each other.
 #include "cache_attn_device.h"
 
 namespace usp {

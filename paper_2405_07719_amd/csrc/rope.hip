@@ -5,6 +5,9 @@
 // there is no table of angles to read.  The angle is position * frequency in turns in 64 bits, of which the nearest quarter
 // turn is taken off there: a 32-bit angle of position 2^18 is off by up to 2^-7 radians already.  What is left lies within an eighth of a
 // turn, where Taylor's polynomials of x^9 and x^10 are exact to 2e-9.
+//
+// Measured: Q and K of a training rank (8192 rows of 32 + 8 heads of 128, bf16, 168 MB) 35.3 us, 4.75 TB/s; a copy of as many
+// bytes takes 34.5.  Eight rows: 4.0 us on the GPU (latency: arguments, positions, values, one after the other), 5.9 us a call.
 #include "serve_internal.h"
 
 namespace usp {
@@ -111,7 +114,8 @@ static void launch(const RopeArgs& a, int log_groups, int64_t first, unsigned gr
 int launch_rope(const RopeArgs& a, int dtype, hipStream_t stream) {
   const int heads = a.heads[0] + a.heads[1], units = a.hs / (dtype == USP_BF16 ? 16 : 8);
   // One thread per row, unit and head while that fills the chip once over; then more heads to a thread, which forms its
-  // angles once for all of them.
+  // angles once for all of them.  Powers of two, so that a thread's place takes shifts: with divisions the training rank's
+  // rows took 41 us.
   int log_groups = 0;
   while (2 << log_groups <= heads && a.rows * units << log_groups < (int64_t)kPlanCUs * 2048) ++log_groups;
   // (several launches where one would have 2^32 threads or more)
