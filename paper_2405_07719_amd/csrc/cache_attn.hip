@@ -15,8 +15,8 @@
 // operand of the second product, whose V operand is 16 bytes of one column of a V tile.  Codes go from memory to registers to
 // the matrix cores, not through LDS.
 //
-// HBM-bound where there is much to read: 64 requests of 256 to 32768 tokens (8 KV heads of 128, 907 MB) 169 us, 5.4 TB/s, one of
-// 212993 tokens (436 MB) 87 us, 5.0 TB/s with both launches; a large copy reaches 4.9.  A wave has the codes of one step in
+// HBM-bound where there is much to read: 64 requests of 256 to 32768 tokens (8 KV heads of 128, 907 MB) 156 us, 5.8 TB/s, one of
+// 212993 tokens (436 MB) 83 us, 5.3 TB/s with both launches; a large copy by the library reaches 4.9.  A wave has the codes of one step in
 // flight, 16 KB, and a CU eight waves.  Short caches are bound by latency: one request of 1003 tokens 8.0 us and 4.5 us for
 // the joining launch (lengths, pages, codes, two products, partial results: one after the other).  12 waves to a CU at head size
 // 64 were no faster (27.7 against 26.4 us for 20 requests of up to 6007 tokens).
@@ -36,7 +36,8 @@ __device__ inline float group_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-template <int HS>
+// ONCE: codes are read by one tile of rows alone, and so past the caches.
+template <int HS, bool ONCE>
 struct Walk {
   static constexpr int KI = HS / 32, ET = HS / 16, KV16 = HS / 64;     // KV16: 16-byte reads of a K row's quarter
   // A partial result in LDS: m and l of each row, then O, rows 16 bytes further apart than in memory (banks).
@@ -59,6 +60,7 @@ struct Walk {
     number_k = cache_counts(bk, vis, nk, p.a.pages) ? nk : -1;
     number_v = cache_counts(bv, vis, nv, p.a.pages) ? nv : -1;
   }
+  __device__ static u32x4 read(const u32x4* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; }
   __device__ void load_k(int step, int head) {
     const int inside = ((step * 4 + (c >> 2)) * 16) & ((1 << p.a.page_shift) - 1);
     const int64_t place = (int64_t)(number_k < 0 ? 0 : number_k) * p.a.hk + head;
@@ -66,7 +68,7 @@ struct Walk {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int i = 0; i < KV16; ++i) k[t][i] = *(const u32x4*)(at + t * 4 * HS + i * 16);
+      for (int i = 0; i < KV16; ++i) k[t][i] = read((const u32x4*)(at + t * 4 * HS + i * 16));
     ks = p.a.k_scale[place];
   }
   __device__ void load_v(int step, int head) {
@@ -74,7 +76,7 @@ struct Walk {
     const int64_t place = (int64_t)(number_v < 0 ? 0 : number_v) * p.a.hk + head;
     const uint8_t* const at = p.a.v_codes + ((place << p.a.page_shift) + inside) * HS + c * 16;
 #pragma unroll
-    for (int e = 0; e < ET; ++e) v[e] = *(const u32x4*)(at + e * 256);
+    for (int e = 0; e < ET; ++e) v[e] = read((const u32x4*)(at + e * 256));
     vs = p.a.v_scale[place];
   }
 
@@ -255,13 +257,13 @@ struct Sum {
 };
 
 template <int HS, typename I> struct Lds {
-  alignas(16) float slot[2 * kWaves][Walk<HS>::kLdsSlot];     // of each wave: the end of a unit, the beginning of one
+  alignas(16) float slot[2 * kWaves][Walk<HS, true>::kLdsSlot];     // of each wave: the end of a unit, the beginning of one
   int first[kWaves];                                          // as in CacheLeft, of a wave's share
   CacheLeft end[kWaves];
   Shares<kThreads, I> shares;
 };
 
-template <int HS, typename I>
+template <int HS, bool ONCE, typename I>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
   extern __shared__ __attribute__((aligned(16))) char dynamic[];
   Lds<HS, I>& lds = *(Lds<HS, I>*)dynamic;
@@ -277,7 +279,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
   // (rounded up: the first wave has a step wherever the workgroup has one)
   const I n = stop - pos, mine = pos + n / kWaves * wave + (n % kWaves * wave + kWaves - 1) / kWaves,
           next = pos + n / kWaves * (wave + 1) + (n % kWaves * (wave + 1) + kWaves - 1) / kWaves;
-  Walk<HS> walk(p, threadIdx.x & 63);
+  Walk<HS, ONCE> walk(p, threadIdx.x & 63);
   int first = 0, end_rows = 0, end_head = 0, end_tile = 0, end_cu = 0;
   shares.walk(p.a, kTile, mine, next, [&](const CacheUnits<I>& u, int seq, int head, int tile, int s0, int s1, int of) __attribute__((always_inline)) {
     const bool begins = s0 == 0, ends = s1 == of;
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
         }
         const float* const slot = lds.slot[2 * x + (x == w ? begins : 0)];
         const f32x2 ml = ((const f32x2*)slot)[row & (kTile - 1)];
-        const f32x4 o = *(const f32x4*)(slot + 2 * kTile + (row & (kTile - 1)) * Walk<HS>::kLdsRow + e);
+        const f32x4 o = *(const f32x4*)(slot + 2 * kTile + (row & (kTile - 1)) * Walk<HS, ONCE>::kLdsRow + e);
         if (x == w) sum = Sum{ml[0], ml[1], o};
         else sum.add(ml[0], ml[1], o);
       }
@@ -409,7 +411,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan
 
 // Requests of few rows go to the kernel that gives each wave units of its own, which reads the cache again for every 16 rows; the
 // one for many rows has a request's rows up to 256 at once, but a step of it takes as long for one as for all.  Measured with 8
-// KV heads of 128, here / there: 64 requests of 256 to 32768 tokens, 16 rows 169 us, 32 rows 295 / 393, 64 rows 547 / 404; 64
+// KV heads of 128, here / there: 64 requests of 256 to 32768 tokens, 16 rows 156 us, 32 rows 295 / 393, 64 rows 547 / 404; 64
 // of 100 to 4000 tokens, 32 rows 63 / 134, 64 rows 94 / 141; one of 32768 tokens, 32 rows 28 / 38, 64 rows 38 / 40.  So 32 rows, and
 // 64 where the table has room for 8192 tokens at most.
 bool few_rows(int group, int max_q, int64_t most_tokens) {
@@ -417,19 +419,19 @@ bool few_rows(int group, int max_q, int64_t most_tokens) {
 }
 int rows_of(bool few) { return few ? kTile : kCacheRowsTile; }
 
-template <int HS, typename I>
+template <int HS, bool ONCE, typename I>
 int launch_few(const CachePlan& p, hipStream_t stream) {
   static LdsLimitRaised raised;
-  if (!raise_dynamic_lds_limit((const void*)cache_attn_kernel<HS, I>, sizeof(Lds<HS, I>), raised)) return USP_ERR_LAUNCH;
-  cache_attn_kernel<HS, I><<<dim3(p.workers), kThreads, sizeof(Lds<HS, I>), stream>>>(p);
+  if (!raise_dynamic_lds_limit((const void*)cache_attn_kernel<HS, ONCE, I>, sizeof(Lds<HS, I>), raised)) return USP_ERR_LAUNCH;
+  cache_attn_kernel<HS, ONCE, I><<<dim3(p.workers), kThreads, sizeof(Lds<HS, I>), stream>>>(p);
   return USP_OK;
 }
-template <int HS>
+template <int HS, bool ONCE>
 int launch_few(const CachePlan& p, hipStream_t stream) {
   const CacheAttnArgs& a = p.a;
   // steps that there can be: tiles, each of the steps of a full table and of one more for each tile before it
   const double tiles = (double)a.total_q * a.group / kTile + a.n_seqs, steps = (double)((int64_t)a.max_pages << a.page_shift) / kStep + 2 + tiles;
-  return tiles * steps * a.hk < 2e9 ? launch_few<HS, int32_t>(p, stream) : launch_few<HS, int64_t>(p, stream);
+  return tiles * steps * a.hk < 2e9 ? launch_few<HS, ONCE, int32_t>(p, stream) : launch_few<HS, ONCE, int64_t>(p, stream);
 }
 
 }  // namespace
@@ -447,7 +449,12 @@ int launch_cache_attn(const CacheAttnArgs& a, int max_q, hipStream_t stream) {
   // Rows of the table that hold 4096 tokens at most, and a unit and more for every CU: a wave has eight steps of a unit at most, and
   // the joining launch would cost more than cutting units between workgroups gains.
   p.whole = few && most_tokens <= 4096 && (int64_t)a.n_seqs * a.hk >= kPlanCUs;
-  const int st = !few ? launch_cache_attn_rows(p, stream) : a.hs == 128 ? launch_few<128>(p, stream) : launch_few<64>(p, stream);
+  // Tiles of one request walk the same codes: where there are several, the caches are to keep them (64 requests of 100 to 4000
+  // tokens, 32 rows: 63 us, past the caches 78); one tile reads them once (64 requests of up to 32768, 16 rows: 170, so 156).
+  const bool once = (int64_t)a.group * max_q <= kTile;
+  const int st = !few ? launch_cache_attn_rows(p, stream)
+                 : a.hs == 128 ? (once ? launch_few<128, true>(p, stream) : launch_few<128, false>(p, stream))
+                               : (once ? launch_few<64, true>(p, stream) : launch_few<64, false>(p, stream));
   if (st != USP_OK) return st;
   if (!p.whole) {
     const dim3 grid(kPlanCUs * 4);

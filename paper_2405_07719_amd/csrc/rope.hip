@@ -6,8 +6,9 @@
 // turn is taken off there: a 32-bit angle of position 2^18 is off by up to 2^-7 radians already.  What is left lies within an eighth of a
 // turn, where Taylor's polynomials of x^9 and x^10 are exact to 2e-9.
 //
-// Measured: Q and K of a training rank (8192 rows of 32 + 8 heads of 128, bf16, 168 MB) 35.3 us, 4.75 TB/s; a copy of as many
-// bytes takes 34.5.  Eight rows: 4.0 us on the GPU (latency: arguments, positions, values, one after the other), 5.9 us a call.
+// Measured: Q and K of a training rank (8192 rows of 32 + 8 heads of 128, bf16, 168 MB) 33 us, 5.1 TB/s; a copy of as many
+// bytes by the library takes 34.5.  Values are read nontemporally, which makes 37 us 33; written so, too, 34, and interleaved
+// pairs in fp32, whose lines two stores share, 44 instead of 35.  Eight rows: 4.0 us on the GPU (latency: arguments, positions, values, one after the other), 5.9 us a call.
 #include "serve_internal.h"
 
 namespace usp {
@@ -76,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int log_grou
     const int t = h >= a.heads[0], ht = t ? h - a.heads[0] : h;
     const T* x = (const T*)a.x[t] + row * a.stride[t] + ht * HS;
     T* y = (T*)a.y[t] + row * a.out_stride[t] + ht * HS;
-    V va = *(const V*)(x + e0), vb = *(const V*)(x + e1);
+    V va = __builtin_nontemporal_load((const V*)(x + e0)), vb = __builtin_nontemporal_load((const V*)(x + e1));
     if (turns) {
       const W fa = __builtin_convertvector(va, W), fb = __builtin_convertvector(vb, W);
       W ga, gb;
