@@ -422,7 +422,7 @@ int usp_cache_append(const usp_cache* c, const void* k, const void* v, const int
  *   different pages: keys of a page whose number is outside [0, pages) are not seen.  A row that sees nothing gets o = 0 and
  *   lse = -inf.  Rows of no request are left as they were.  What stands in the cache behind kv_len has no influence.
  *   max_q: the most rows of any request, as far as the caller knows; only speed depends on it.  total_q = 0 or n_seqs = 0 does
- *   nothing.  kv_len is taken as 0 .. max_pages * page.  scale = 0 means 1/sqrt(hs).
+ *   nothing.  kv_len is taken as 0 .. max_pages * page (and less than 2^31 - 127).  scale = 0 means 1/sqrt(hs).
  * The workspace (DEVICE, 16-byte aligned; its size depends on hq / hk, hs and max_q alone) holds partial results of the call;
  * calls that overlap in time need one each.  Nothing in it has to be cleared or kept.  Results do not depend on the order in
  * which workgroups finish. */

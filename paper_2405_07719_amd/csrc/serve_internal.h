@@ -76,7 +76,7 @@ struct CacheUnits {
     int c0 = a.cu_q[i], c1 = a.cu_q[i + 1];
     c0 = c0 < 0 ? 0 : c0 > total ? total : c0;
     c1 = c1 < c0 ? c0 : c1 > total ? total : c1;
-    const int64_t room = (int64_t)a.max_pages << a.page_shift;
+    const int64_t most = INT32_MAX & ~127, all = (int64_t)a.max_pages << a.page_shift, room = all < most ? all : most;   // (the end of the last step fits)
     const int x = a.kv_len[i];
     return Request{c0, c1 - c0, x < 0 ? 0 : x > room ? (int)room : x};
   }

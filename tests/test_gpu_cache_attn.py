@@ -29,15 +29,16 @@ class Case:
             q = wide[:, :hq]
         self.q = q
 
-    def run(self, max_q=None, workspace=None, scale=0.0):
+    def run(self, max_q=None, workspace=None, scale=0.0, table=None):
         hs, n = self.cache.hs, len(self.lens)
+        table = sl.ints(self.table) if table is None else table
         o = torch.full((self.total, self.hq, hs), 7.0, dtype=sl.torch_dtype(self.o_dtype), device="cuda")
         lse = torch.full((self.hq, self.total), 7.0, device="cuda")
         max_q = int(np.diff(self.cu).max()) if max_q is None else max_q
         ws = workspace
         if ws is None:      # what stood in it before must not matter
             ws = torch.full((self.usp.usp_cache_attn_workspace_bytes(self.cache.c, self.hq, max_q),), 0xff, dtype=torch.uint8, device="cuda")
-        self.usp.usp_cache_attn(self.cache.c, self.q, self.q.stride(0), sl.ints(self.cu), sl.ints(self.lens), sl.ints(self.table), self.table.shape[1],
+        self.usp.usp_cache_attn(self.cache.c, self.q, self.q.stride(0), sl.ints(self.cu), sl.ints(self.lens), table, table.shape[1],
                                 n, self.total, max_q, self.hq, scale, self.causal, o, lse, self.o_dtype, ws)
         return o, lse
 
@@ -254,6 +255,19 @@ def test_two_streams_two_workspaces_and_graphs(usp):
         k, v = a.cache.values()
         ref = sl.attention(sl.f64(a.q), k, v, a.cu, np.maximum(a.lens - shorter, 0), a.table, 64, a.cache.pages, True)
         sl.check_attention(sl.f64(o), sl.f64(lse), ref, sl.BF16)
+
+
+@pytest.mark.parametrize("hs", [64, 128])
+@pytest.mark.parametrize("news", [[1, 1, 1, 1], [3, 1, 8, 2]])
+def test_tables_whose_steps_pass_32_bits(usp, hs, news):
+    """Rows of the table for 2^31 tokens: steps are counted in 64 bits, whatever the lengths are."""
+    case = Case(usp, 71 + hs, [3000, 77, 900, 1], news, 16, 16, hs, 128)
+    want = case.check()
+    table = torch.full((4, 1 << 24), -1, dtype=torch.int32, device="cuda")
+    table[:, :case.table.shape[1]] = sl.ints(case.table)
+    o, lse = case.run(table=table)
+    sl.check_attention(sl.f64(o), sl.f64(lse), case.reference(), sl.BF16)
+    assert float((o.float() - want[0].float()).abs().max()) < 2e-2
 
 
 def test_a_cache_beyond_32_bits(usp):
