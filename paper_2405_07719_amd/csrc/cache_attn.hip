@@ -93,11 +93,11 @@ struct Walk {
     const int32_t* const row = a.block_table + (int64_t)seq * a.max_pages;
     rows = u.rows(a, tile, kTile);
     // keys that the tile's first and last rows see
-    const int64_t row_first = (int64_t)tile * kTile;
-    const int vis = u.seen_by((row_first + rows - 1) / a.group), vis_first = u.seen_by(row_first / a.group);
-    const int in = (int)((row_first + c) / a.group), limit = c < rows ? u.seen_by(in) : vis;
+    const uint32_t row_first = (uint32_t)tile * kTile, group = (uint32_t)a.group;
+    const int vis = u.seen_by((row_first + rows - 1) / group), vis_first = u.seen_by(row_first / group);
+    const int in = (int)((row_first + c) / group), limit = c < rows ? u.seen_by(in) : vis;
     token = u.cu + in;
-    hq = head * a.group + (int)(row_first + c - (int64_t)in * a.group);
+    hq = head * a.group + (int)(row_first + c - (uint32_t)in * group);
     m = -INFINITY;
     l = 0.0f;
     const __bf16* const from = (const __bf16*)a.q + (int64_t)token * a.q_stride + hq * HS + g * (HS / 4);
@@ -246,8 +246,8 @@ struct Sum {
   }
   // row `row` of a unit's request and KV head, columns e .. e + 3
   template <int HS>
-  __device__ void write(const CacheAttnArgs& a, const CacheLeft& unit, int64_t row, int e) const {
-    const int in = (int)(row / a.group), hq = unit.head * a.group + (int)(row - (int64_t)in * a.group), token = unit.cu + in;
+  __device__ void write(const CacheAttnArgs& a, const CacheLeft& unit, uint32_t row, int e) const {
+    const int in = (int)(row / (uint32_t)a.group), hq = unit.head * a.group + (int)(row - (uint32_t)in * a.group), token = unit.cu + in;
     const f32x4 y = o * (l == 0.0f ? 0.0f : 1.0f / l);
     const int64_t to = ((int64_t)token * (a.hk * a.group) + hq) * HS + e;
     if (a.o_dtype == USP_BF16) *(bf16x4*)((__bf16*)a.o + to) = __builtin_convertvector(y, bf16x4);
@@ -324,7 +324,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn_kernel(CachePlan p) {
       }
       if (begins && ended) {
         const CacheLeft& unit = lds.end[w];
-        if (row < unit.rows) sum.template write<HS>(p.a, unit, (int64_t)unit.tile * kTile + row, e);
+        if (row < unit.rows) sum.template write<HS>(p.a, unit, (uint32_t)unit.tile * kTile + row, e);
       } else {
         float* const to = slots + (begins ? CachePlan::slot(kTile, HS) : 0);
         if (row < kTile) {
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_attn_join_kernel(CachePlan
       if (from == 0)
         for (int t = team + 1; t < team + share; ++t) sum.add(mls[t][0], mls[t][1], sums[t][tid % kTeam]);
     }
-    if (real && from == 0) sum.template write<HS>(a, unit, (int64_t)unit.tile * rows_per_tile + row, e);
+    if (real && from == 0) sum.template write<HS>(a, unit, (uint32_t)unit.tile * rows_per_tile + row, e);
   }
 }
 

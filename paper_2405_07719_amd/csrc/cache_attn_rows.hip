@@ -237,14 +237,14 @@ struct RowsWalk {
   __device__ __forceinline__ void unit(const CacheUnits<>& u, int seq, int head, int tile, int s0, int s1, bool whole, float* slot) {
     const int32_t* const row = a.block_table + (int64_t)seq * a.max_pages;
     const int rows = u.rows(a, tile, kCacheRowsTile);
-    const int64_t row_first = (int64_t)tile * kCacheRowsTile;
-    const int vis = u.seen_by((row_first + rows - 1) / a.group);
+    const uint32_t row_first = (uint32_t)tile * kCacheRowsTile, group = (uint32_t)a.group;
+    const int vis = u.seen_by((row_first + rows - 1) / group);
     const int end = (vis + kStep - 1) / kStep < s1 ? (vis + kStep - 1) / kStep : s1;
     const int mine = wave * kRows + c, wave_rows = rows - wave * kRows < kRows ? rows - wave * kRows : kRows;
-    const int64_t row_wave = row_first + wave * kRows;
-    const int token = (int)((row_first + mine) / a.group), hq = head * a.group + (int)(row_first + mine - (int64_t)token * a.group);
-    vis_wave = wave_rows > 0 ? __builtin_amdgcn_readfirstlane(u.seen_by((row_wave + wave_rows - 1) / a.group)) : 0;
-    vis_first = wave_rows > 0 ? __builtin_amdgcn_readfirstlane(u.seen_by(row_wave / a.group)) : 0;
+    const uint32_t row_wave = row_first + wave * kRows;
+    const int token = (int)((row_first + mine) / group), hq = head * a.group + (int)(row_first + mine - (uint32_t)token * group);
+    vis_wave = wave_rows > 0 ? __builtin_amdgcn_readfirstlane(u.seen_by((row_wave + wave_rows - 1) / group)) : 0;
+    vis_first = wave_rows > 0 ? __builtin_amdgcn_readfirstlane(u.seen_by(row_wave / group)) : 0;
     limit = mine < rows ? u.seen_by(token) : vis_wave;
     m = -INFINITY;
     l = 0.0f;

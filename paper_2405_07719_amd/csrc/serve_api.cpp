@@ -257,6 +257,7 @@ extern "C" int usp_cache_attn(const usp_cache* c, const void* q, int64_t q_strid
   if (n_seqs < 0 || total_q < 0 || max_q < 0 || max_pages < 1 || hq < 1) return USP_ERR_SHAPE;
   if (hq % c->hk) return USP_ERR_DEGREE;
   if (n_seqs > USP_CACHE_MAX_REQUESTS || hq / c->hk > 65536 || total_q >= (int64_t)1 << 31) return USP_ERR_UNSUPPORTED;
+  if (total_q * (hq / c->hk) >= ((int64_t)1 << 32) - 256) return USP_ERR_UNSUPPORTED;   // rows of a KV head are counted in 32 bits
   if (o_dtype != USP_BF16 && o_dtype != USP_FP32) return USP_ERR_DTYPE;
   if (!(scale >= 0.0f) || isinf(scale)) return USP_ERR_UNSUPPORTED;
   if (n_seqs == 0 || total_q == 0) return USP_OK;

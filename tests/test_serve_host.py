@@ -117,7 +117,7 @@ def test_cache_refusals(lib):
     att = lambda c=None, q=A + (4 << 30), qs=1024, cu=A + (5 << 30), lens=A + (6 << 30), table=A + (7 << 30), mp=4, n=2, total=2, mq=1, hq=8, scale=0.0, o=A + (8 << 30), lse=A + (9 << 30), dt=0, ws=A + (10 << 30), room=need: (  # noqa: E731
         usp.usp_cache_attn(c or cache(), q, qs, cu, lens, table, mp, n, total, mq, hq, scale, True, o, lse, dt, ws, room, 0))
     for status, kw in ((2, dict(n=-1)), (2, dict(total=-1)), (2, dict(mq=-1)), (2, dict(mp=0)), (2, dict(hq=0)), (3, dict(hq=7)), (6, dict(n=8193)),
-                       (6, dict(total=1 << 31)), (4, dict(dt=2)), (6, dict(scale=-1.0)), (6, dict(scale=float("nan"))), (6, dict(scale=float("inf"))),
+                       (6, dict(total=1 << 31)), (6, dict(total=(1 << 31) - 1, hq=64)), (4, dict(dt=2)), (6, dict(scale=-1.0)), (6, dict(scale=float("nan"))), (6, dict(scale=float("inf"))),
                        (1, dict(q=None)), (1, dict(lse=None)), (1, dict(table=None)), (2, dict(qs=1016)), (6, dict(qs=1028)), (6, dict(q=A + 8)),
                        (6, dict(o=A + (8 << 30) + 2)), (5, dict(ws=None)), (5, dict(room=need - 1)), (6, dict(ws=A + (10 << 30) + 4)),
                        (6, dict(o=A + (4 << 30))), (6, dict(c=cache(hs=256)))):
