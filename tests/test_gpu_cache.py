@@ -23,7 +23,7 @@ def extend(usp, cu, before, total, table, page, pages, free, max_pages=None):
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
-@pytest.mark.parametrize("n,most", [(1, 1), (1, 5000), (3, 1), (255, 3), (256, 1), (257, 90), (1000, 2), (2100, 40)])
+@pytest.mark.parametrize("n,most", [(1, 1), (1, 5000), (3, 1), (255, 3), (256, 1), (257, 90), (1000, 2), (2100, 40), (6100, 1), (8192, 3)])
 def test_extend(usp, page, n, most):
     rng = np.random.default_rng(n + most + page)
     before = np.where(rng.random(n) < 0.2, 0, rng.integers(0, 700, n))

@@ -119,6 +119,21 @@ def test_many_requests(usp, n):
             Case(usp, n, lens.tolist(), rng.choice([0, 1, 1, 1, 2], n).tolist(), 4, 2, 64, 16, wide=wide).check(max_q=most)
 
 
+def test_as_many_requests_as_there_may_be(usp):
+    rng = np.random.default_rng(8192)
+    lens = rng.integers(0, 40, 8192)
+    Case(usp, 81, lens.tolist(), rng.choice([0, 1, 1, 2], 8192).tolist(), 2, 1, 64, 16, o_dtype=sl.FP32).check(max_q=2)
+
+
+@pytest.mark.parametrize("most", [1, 1000])
+def test_requests_that_share_pages(usp, most):
+    """A prefix that several requests have in common, and a table row that names one page again and again."""
+    case = Case(usp, 82, [200, 180, 130], [1, 40, 3], 8, 2, 128, 16)
+    case.table[1, :8] = case.table[0, :8]
+    case.table[2, :] = case.table[2, 0]
+    case.check(max_q=most)
+
+
 def test_the_most_rows_are_a_hint(usp):
     """max_q below and above what the requests have: the same attention."""
     case = Case(usp, 3, [500, 90, 1200], [1, 30, 9], 8, 2, 128, 64)
