@@ -10,10 +10,10 @@
 // leaves: of 16 tokens of V the lanes below 32 need 0-3 and 8-11, the others 4-7 and 12-15, which is the order in which they
 // are written to LDS.
 //
-// Step s puts the codes of K two steps ahead and of V one step ahead, which came during the step before, into LDS and asks for
+// Step s puts the codes of K three steps ahead and of V two steps ahead, which came during the step before, into LDS and asks for
 // those behind them; then, side by side, the scores of step s + 1 and the products with V of step s (matrix cores), the
-// exponentials of step s and the maxima of step s + 1 (vector ALU).  K and V have two buffers each, and a step ends with the one
-// barrier that they need.
+// exponentials of step s and the maxima of step s + 1 (vector ALU).  K and V have four buffers each, so that only every
+// second step ends with a barrier (two buffers and a barrier at every step: 1 % slower with full tiles, 3 to 5 % with a few rows).
 //
 // Measured: 4096 rows of 32 heads over 49152 tokens (3.16 TFLOP) 2.8 ms, 1.11 to 1.15 PFLOP/s, matrix cores busy 55 % of the
 // cycles; a library product of 8192 x 8192 matrices reaches 1.11, of 16384 1.37.  Without the exponentials, or without bringing
@@ -23,20 +23,20 @@
 namespace usp {
 namespace {
 
-constexpr int kThreads = 512, kStep = kCacheStep, kRows = 32, kLeastSteps = 4;
+constexpr int kThreads = 512, kStep = kCacheStep, kRows = 32, kLeastSteps = 4, kBuffers = 4;
 
 template <int HS> constexpr int k_stride() { return HS * 2 + 16; }
 constexpr int kVStride = kStep * 2 + 16;
 template <int HS> constexpr int k_bytes() { return kStep * k_stride<HS>(); }
 template <int HS> constexpr int v_bytes() { return HS * kVStride; }
-// Beside K and V, for each of the two buffers: which of a step's 16-token blocks have no page (a byte each), whether a wave brought
+// Beside K and V, for each buffer: which of a step's 16-token blocks have no page (a byte each), whether a wave brought
 // NaN values (a byte each), and where they are (16 bits for each column and block).
 struct Marks { uint8_t missing[4], unused[4], nan[kThreads / 64]; };
 template <int HS> struct Lds {
-  alignas(16) char k[2][k_bytes<HS>()];
-  alignas(16) char v[2][v_bytes<HS>()];
-  alignas(16) Marks marks[2];
-  alignas(8) uint16_t nan[2][HS][4];
+  alignas(16) char k[kBuffers][k_bytes<HS>()];
+  alignas(16) char v[kBuffers][v_bytes<HS>()];
+  alignas(16) Marks marks[kBuffers];
+  alignas(8) uint16_t nan[kBuffers][HS][4];
   Shares<kThreads, int64_t> shares;
 };
 
@@ -115,7 +115,7 @@ struct RowsWalk {
     to[0] = widened(y[0], y[2], scale);
     to[1] = widened(y[1], y[3], scale);
   }
-  // Marks of both buffers as put_v expects to find them.
+  // Marks of all buffers as put_v expects to find them.
   __device__ void clear_marks() const {
     if (tid < (int)(sizeof(lds.marks) / 4)) ((uint32_t*)lds.marks)[tid] = 0;
     for (int i = tid; i < (int)(sizeof(lds.nan) / 4); i += kThreads) ((uint32_t*)lds.nan)[i] = 0;
@@ -150,7 +150,7 @@ struct RowsWalk {
   __device__ __forceinline__ void operands(int s, int n, bf16x8 (&f)[2]) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      f[i] = n < KS ? k_operand((s + 1) & 1, i, n) : v_operand(s & 1, (n - KS) % (EB / 2) * 2 + i, (n - KS) / (EB / 2));
+      f[i] = n < KS ? k_operand((s + 1) % kBuffers, i, n) : v_operand(s % kBuffers, (n - KS) % (EB / 2) * 2 + i, (n - KS) / (EB / 2));
   }
   // How many of a step's 32 weights are formed before group n.
   static constexpr int weights_before(int n) { return n <= KS ? 24 * n / KS : n - KS >= EB ? 32 : 24 + 8 * (n - KS) / EB; }
@@ -229,7 +229,7 @@ struct RowsWalk {
       for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (*(const uint64_t*)lds.nan[s & 1][eb * 32 + 8 * (i / 4) + 4 * h + i % 4] & seen) o[eb][i] = NAN;
+          if (*(const uint64_t*)lds.nan[s % kBuffers][eb * 32 + 8 * (i / 4) + 4 * h + i % 4] & seen) o[eb][i] = NAN;
     }
   }
 
@@ -256,33 +256,39 @@ struct RowsWalk {
     if (s0 < end) {
       const auto at_most = [&](int s) { return s < end ? s : end - 1; };
       const auto block_of = [&](int s) { return found(number(row, at_most(s), vis), at_most(s), vis, head); };
-      const Block b0 = block_of(s0), b1 = block_of(s0 + 1);
-      Block bk = block_of(s0 + 3), bv = block_of(s0 + 2);      // of the codes that are asked for next
-      int ahead = number(row, at_most(s0 + 4), vis), left;     // left: tokens of the V block that is on its way
+      const Block b0 = block_of(s0), b1 = block_of(s0 + 1), b2 = block_of(s0 + 2);
+      Block bk = block_of(s0 + 4), bv = block_of(s0 + 3);      // of the codes that are asked for next
+      int ahead = number(row, at_most(s0 + 5), vis), left;     // left: tokens of the V block that is on its way
       Piece kk = {}, vv = {};
       {
-        Piece k0 = {}, k1 = {}, v0 = {};
+        Piece k0 = {}, k1 = {}, k2 = {}, v0 = {}, v1 = {};
         if (brings_k()) {
           k0 = load(a.k_codes, a.k_scale, b0);
           k1 = load(a.k_codes, a.k_scale, b1);
+          k2 = load(a.k_codes, a.k_scale, b2);
           kk = load(a.k_codes, a.k_scale, bv);
         }
         if (brings_v()) {
           v0 = load(a.v_codes, a.v_scale, b0);
-          vv = load(a.v_codes, a.v_scale, b1);
+          v1 = load(a.v_codes, a.v_scale, b1);
+          vv = load(a.v_codes, a.v_scale, b2);
         }
-        left = b1.left;
+        left = b2.left;
         __syncthreads();                            // the unit before has been read
         if (brings_k()) {
-          put_k(k0, s0 & 1);
-          put_k(k1, (s0 + 1) & 1);
+          put_k(k0, s0 % kBuffers);
+          put_k(k1, (s0 + 1) % kBuffers);
+          put_k(k2, (s0 + 2) % kBuffers);
         }
-        if (brings_v()) put_v(v0, s0 & 1, b0.left, marked);
+        if (brings_v()) {
+          put_v(v0, s0 % kBuffers, b0.left, marked);
+          put_v(v1, (s0 + 1) % kBuffers, b1.left, marked);
+        }
       }
       __syncthreads();
       f32x16 x[2], y[2];
-      scores(s0 & 1, x);
-      __syncthreads();                              // (the first step's scores have been formed: its K makes room below)
+      scores(s0 % kBuffers, x);
+      __syncthreads();                              // (the first step's scores have been formed: its K makes room in the second step)
       float top = x[0][0];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -290,21 +296,19 @@ struct RowsWalk {
         for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
       int s = s0;
       const auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2]) __attribute__((always_inline)) {
-        const u32x4 marks = *(const u32x4*)&lds.marks[s & 1];
-        if (brings_k()) put_k(kk, s & 1);           // of step s + 2
-        if (brings_v()) put_v(vv, (s + 1) & 1, left, marked);
+        const u32x4 marks = *(const u32x4*)&lds.marks[s % kBuffers];
+        if (brings_k()) put_k(kk, (s + 3) % kBuffers);
+        if (brings_v()) put_v(vv, (s + 2) % kBuffers, left, marked);
         if (brings_k()) kk = load(a.k_codes, a.k_scale, bk);
         if (brings_v()) vv = load(a.v_codes, a.v_scale, bv);
         left = bv.left;
         bv = bk;
-        bk = found(ahead, at_most(s + 4), vis, head);
-        ahead = number(row, at_most(s + 5), vis);
+        bk = found(ahead, at_most(s + 5), vis, head);
+        ahead = number(row, at_most(s + 6), vis);
         if (s * kStep < vis_wave) compute(s, marks, now, next, top);
-        __syncthreads();
         return ++s < end;
       };
-      while (step(x, y) && step(y, x)) {
-      }
+      while (step(x, y) && step(y, x)) __syncthreads();
     }
     l += __shfl_xor(l, 32);
     if (mine >= rows) return;
