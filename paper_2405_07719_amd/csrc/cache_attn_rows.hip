@@ -308,6 +308,8 @@ struct RowsWalk {
         if (s * kStep < vis_wave) compute(s, marks, now, next, top);
         return ++s < end;
       };
+      // Two steps from s on read K of s + 1 and s + 2 and V of s and s + 1, and write K of s + 3 and s + 4 and V of s + 2 and s + 3: other
+      // buffers, of four each.
       while (step(x, y) && step(y, x)) __syncthreads();
     }
     l += __shfl_xor(l, 32);
